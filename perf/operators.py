@@ -46,8 +46,10 @@ def _quant(name, m, k, *, gate, pad=0):
     return dict(c, name=name) if name else c
 
 
-def _linear(name, m, n, k, pad=0):
-    c = dict(kind="linear", m=m, n=n, k=k, pad=pad)
+def _linear(name, m, n, k, pad=0, by_row=False):
+    """``by_row``: the activations' scales lie row by row, and not as the library's
+    own quantization leaves them (the scales of a block of K side by side)."""
+    c = dict(kind="linear", m=m, n=n, k=k, pad=pad, by_row=by_row)
     return dict(c, name=name) if name else c
 
 
@@ -74,7 +76,7 @@ def listed():
         # a decode batch through the query, key and value projection
         _linear("linear_decode", 48, 6144, 4096),
         # a verify batch of odd size into a width off every tile, K in half blocks
-        _linear("linear_ragged", 333, 5000, 2112),
+        _linear("linear_ragged", 333, 5000, 2112, by_row=True),
         # prefill: the query, key and value projection, and a wide model's MLP
         _linear("linear_prefill", 4096, 6144, 4096),
         _linear("linear_wide", 4096, 28672, 8192),
@@ -120,7 +122,7 @@ def draw(rng):
         if rng.random() < 0.8:
             k = max(128, k // 128 * 128)
         if 2.0 * m * n * k <= 1.9e12:
-            return _linear(None, m, n, k, rng.choice([0, 0, 16, 64]))
+            return _linear(None, m, n, k, rng.choice([0, 0, 16, 64]), rng.random() < 0.25)
 
 
 # ---------------------------------------------------------------------------
@@ -205,8 +207,9 @@ def _linear_inputs(case, seed):
     b, bs = _to_blocks(_normal(gen, (n, k), 0.02).float())
     a = torch.empty((m, k + case["pad"]), dtype=E4M3, device="cuda")
     a.copy_((_normal(gen, (m, k + case["pad"])) * 120.0).clamp_(-448.0, 448.0))
-    s = torch.empty((m, kb), dtype=torch.float32, device="cuda")
+    s = torch.empty((m, kb) if case["by_row"] else (kb, m), dtype=torch.float32, device="cuda")
     s.uniform_(0.002, 0.02, generator=gen)
+    s = s if case["by_row"] else s.t()
     return dict(a=a[:, :k], a_s=s, b=b, b_s=bs)
 
 
