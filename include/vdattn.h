@@ -294,6 +294,45 @@ int vd_kv_write(const vd_attn* h, const void* k_new, const void* v_new,
                 const int64_t* slot_mapping, int64_t num_tokens, void* k_pool, void* v_pool,
                 int64_t num_pages, hipStream_t stream);
 
+/* The page map of one call, made on the device from the request lengths: what
+ * vd_attn_forward (cu_q_lens, context_lens, page_table) and vd_kv_write (slot_mapping) take.
+ * Request r has q_lens[r] = s new tokens and cached_lens[r] = c tokens in the cache; n = c + s.
+ *   cu_q_lens[r + 1] = sum_{i <= r} max(s_i, 0), cu_q_lens[0] = 0 (values past 2^31 - 1 as that)
+ *   context_lens[r] = n
+ *   the request's pages ceil(c / 16) .. ceil(n / 16) - 1 are the next ones of free_pages, in
+ *   request order, and are written into its row of page_table (other entries are left as they
+ *   were: the pages of the cached tokens have to be there, and the page that holds token c,
+ *   where c mod 16 > 0, has to be the request's own); *pages_used: how many were taken
+ *   slot_mapping[t] = page * 16 + p mod 16 of row t's position p = c + (t - cu_q_lens[r]); -1 for
+ *   the rows behind the last request and where the page id is outside [0, num_pages)
+ *   status[r]: 0, or the bit mask of why the request is refused:
+ *     1  s < 0, c < 0 or n > 2^31 - 1;      2  ceil(n / 16) > pt_stride;
+ *     4  the free list has too few pages;   8  its rows end past total_q_tokens.
+ * A refused request takes no page, its table row is left as it was, its context_lens is 0 (the
+ * attention skips it) and its rows' slots are -1 (the KV write skips them).  A request without
+ * new tokens (s = 0) is not refused; the attention skips it.
+ * All pointers are device memory, int32 arrays 4-byte and slot_mapping 8-byte aligned.  The
+ * outputs overlap nothing else (context_lens or status == cached_lens or q_lens:
+ * VD_ERR_INVALID_ARG).  One launch on `stream`, no workspace; it may be captured, and a replay
+ * reads the lengths that are there then. */
+typedef struct {
+  int32_t num_seqs;            /* B >= 0 */
+  int64_t total_q_tokens;      /* rows of slot_mapping, 0 .. 2^31 - 4097; may be more than sum s */
+  const int32_t* q_lens;       /* [B] */
+  const int32_t* cached_lens;  /* [B] */
+  const int32_t* free_pages;   /* [num_free] page ids */
+  int64_t num_free;            /* >= 0 */
+  int64_t num_pages;           /* >= 0, of the pool */
+  int32_t* page_table;         /* [B * pt_stride], in and out */
+  int32_t pt_stride;           /* >= 1 */
+  int32_t* cu_q_lens;          /* out [B + 1] */
+  int32_t* context_lens;       /* out [B] */
+  int64_t* slot_mapping;       /* out [total_q_tokens] */
+  int32_t* status;             /* out [B] */
+  int32_t* pages_used;         /* out [1] */
+} vd_page_map;
+int vd_map_pages(const vd_page_map* map, hipStream_t stream);
+
 /* Batch-invariant linear layer (the matmul contract of Section 5.4, Fig. 3: the output
  * row of a token depends only on that token's input row and on the weights):
  *   c[m][n] = bf16_RNE( sum_k a[m][k] * b[n][k] )   for 0 <= m < M, 0 <= n < N
@@ -314,6 +353,74 @@ int vd_kv_write(const vd_attn* h, const void* k_new, const void* v_new,
  * returns without waiting; allocates nothing.  Strides are in elements. */
 int vd_linear(const void* a, int64_t lda, const void* b, int64_t ldb, void* c, int64_t ldc,
               int64_t M, int32_t N, int32_t K, hipStream_t stream);
+
+/* The 8-bit operators.  An 8-bit matrix holds e4m3 values (OCP: 4 exponent bits, 3
+ * mantissa bits, largest value 448, no infinity) in rows of K, and fp32 scales, one for
+ * each block of 128 values of a row (the last block of a row may be shorter): the value
+ * (m, k) stands for code[m][k] * scale(m, k / 128).  Scales are given by a pointer and two
+ * strides in floats: scale (m, j) lies at [m * s_row + j * s_blk], 4-byte aligned, for
+ * 0 <= j < ceil(K / 128).  s_row = 1 with s_blk >= M (the scales of one block of K side by
+ * side) is the layout the linear layer reads fastest.  Rows of one matrix must not overlap. */
+
+/* RMS norm with the residual's addition:
+ *   h[m][k] = bf16_RNE(x[m][k] + residual[m][k])      (h = x when residual is NULL)
+ *   y[m][k] = (h[m][k] * (1 / sqrt(sum_k h[m][k]^2 / K + eps))) * weight[k]      in fp32
+ *   sum[m][k] = h[m][k] (only with a residual), out[m][k] = bf16_RNE(y[m][k])
+ * vd_rmsnorm_fp8 writes y in 8 bits instead: of each 128 values of a row,
+ *   scale = max(max |y|, 2^-117) * fl(1 / 448), code = e4m3_RNE(y * (1 / scale)).
+ * A group that holds a NaN or an infinity gets a scale that is not finite, and codes that
+ * stand for NaN throughout.  The bits of a row depend on that row, the weight and eps only
+ * (the sum of squares is one tree fixed by K), so a row normed with its addition equals one
+ * normed after it, and rows do not depend on M.
+ * x, residual, sum, out: device rows of K bf16 values (out of vd_rmsnorm_fp8: K codes);
+ * weight: K bf16 values.  Strides in elements.  residual and sum go together (both NULL:
+ * no addition).  sum may be x or residual and the bf16 out may be x, residual or sum's
+ * input (the same pointer and stride: rows in place); other overlaps are not allowed.
+ * Requirements: K a multiple of 8 and at most 32768 (else VD_ERR_UNSUPPORTED); eps finite,
+ * >= 0; bf16 rows 16-byte aligned with strides >= K that are multiples of 8; codes 8-byte
+ * aligned with a stride >= K that is a multiple of 8; s_row, s_blk >= 1 where M > 1 and
+ * K > 128 (else VD_ERR_INVALID_ARG).  M = 0 or K = 0: nothing to do.  One launch on
+ * `stream`; allocates nothing. */
+int vd_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
+               float eps, void* sum, int64_t lds, void* out, int64_t ldo, int64_t M, int32_t K,
+               hipStream_t stream);
+int vd_rmsnorm_fp8(const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                   const void* weight, float eps, void* sum, int64_t lds, void* out, int64_t ldo,
+                   float* scales, int64_t s_row, int64_t s_blk, int64_t M, int32_t K,
+                   hipStream_t stream);
+
+/* Rows of bf16 in 8 bits, by the rule of vd_rmsnorm_fp8: y = x, or with a gate (not NULL)
+ *   y[m][k] = gate[m][k] / (1 + exp(-gate[m][k])) * x[m][k]      in fp32
+ * (the inner activation of a gated MLP; gate and x may be two column ranges of one matrix).
+ * Requirements as for vd_rmsnorm_fp8, with any K that is a multiple of 8; out overlaps
+ * neither input.  A row's bits depend on that row only. */
+int vd_quantize_fp8(const void* x, int64_t ldx, const void* gate, int64_t ldg, void* out,
+                    int64_t ldo, float* scales, int64_t s_row, int64_t s_blk, int64_t M, int32_t K,
+                    hipStream_t stream);
+
+/* vd_linear on 8-bit matrices:
+ *   c[m][n] = bf16_RNE( sum_j as(m, j) * bs(n / 128, j) * sum_{k in block j} a[m][k] * b[n][k] )
+ * a: device [M rows of lda] e4m3 activations, as: their scales, one per row and block;
+ * b: device [N rows of ldb] e4m3 weights, one row per output feature, bs: their scales, one
+ *    for each block of 128 rows and 128 values of K (bs_row steps 128 output features; any
+ *    strides >= 0);
+ * c: device [M rows of ldc] bf16 output (the first N values of a row written).
+ * Each output element is one fp32 chain over the blocks of K in ascending order: the block's
+ * sum of products by the matrix core (v_mfma_f32_16x16x128_f8f6f4 from +0, which cuts each
+ * product to a multiple of 2^(E - 13), E the largest sum of the factors' exponents among 8
+ * neighbours of K, and adds in fp32), multiplied by
+ * as * bs and added with one rounding (fma), cast to bf16 round-to-nearest-even at the end:
+ * row m of c is bit-identical for any M, any position of the row in a, and any strides.
+ * Requirements (else VD_ERR_UNSUPPORTED for K, VD_ERR_INVALID_ARG otherwise): K a multiple
+ * of 64; when K > 0, lda, ldb >= K and multiples of 16 with a and b 16-byte aligned and
+ * scales 4-byte aligned (K = 0: none of them is read and every output is +0); ldc >= N; c
+ * 2-byte aligned; M, N, K >= 0 (M = 0 or N = 0: nothing to do; VD_ERR_INVALID_ARG past what
+ * one launch covers).  c overlaps no input.  Launches on `stream` and returns without waiting;
+ * allocates nothing.  Strides are in elements. */
+int vd_linear_fp8(const void* a, int64_t lda, const float* a_scales, int64_t as_row,
+                  int64_t as_blk, const void* b, int64_t ldb, const float* b_scales,
+                  int64_t bs_row, int64_t bs_blk, void* c, int64_t ldc, int64_t M, int32_t N,
+                  int32_t K, hipStream_t stream);
 
 /* Static description of a status code (never NULL). */
 const char* vd_status_string(int status);

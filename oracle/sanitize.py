@@ -56,8 +56,9 @@ def build_library(out: str) -> str:
            # host pass only
            "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
            "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer",
-           "-I", os.path.join(ROOT, "include"), os.path.join(CSRC, "vd_attn.hip"),
-           os.path.join(CSRC, "vd_linear.hip"), "-o", out]
+           "-I", os.path.join(ROOT, "include"),
+           *(os.path.join(CSRC, f) for f in ("vd_attn.hip", "vd_linear.hip", "vd_linear_fp8.hip",
+                                             "vd_rows.hip", "vd_pages.hip")), "-o", out]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stderr)

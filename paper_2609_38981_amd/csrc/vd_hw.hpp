@@ -37,6 +37,20 @@ __device__ __forceinline__ void lds_dma16(const void* src, uint32_t m0val) {
       : "memory");
 }
 
+// The same of 4 bytes per lane: lane l's land at LDS byte address m0val + 4 l.
+__device__ __forceinline__ void lds_dma4(const void* src, uint32_t m0val) {
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %1, off\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(src), "s"(m0val)
+      : "memory");
+}
+
 // N direct global-to-LDS copies of 1 KB (N = 2 or 4) with one M0 setting:
 // copy i moves lane l's 16 bytes from src + 1024 i to LDS byte address
 // m0val + 1024 i + 16 l (the instruction's immediate offset moves both the

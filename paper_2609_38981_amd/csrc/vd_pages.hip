@@ -1,0 +1,197 @@
+// vd_pages.hip -- the page map of one call, made on the device from the request
+// lengths (vd_map_pages of libvdattn.so, gfx950): what the engine does between
+// its scheduler and the attention (the paper's Section 4.1: new tokens get
+// private slots, full pages stay where they are).
+//
+// With s new and c cached tokens of request r, n = c + s:
+//   cu_q_lens[r + 1] = sum_{i <= r} s_i
+//   have = ceil(c / 16) pages are in the table already; pages have .. ceil(n / 16) - 1
+//   are the next ones of the free list: first_r = sum_{i < r} (ceil(n_i / 16) - have_i)
+//   token t of request r stands at position p = c + (t - cu_q_lens[r]) and gets the
+//   slot page(floor(p / 16)) * 16 + p mod 16.
+// One launch.  Every workgroup makes both prefix sums of all requests itself (4
+// requests a thread; a call has a few hundred), keeps them in LDS and writes the
+// slots of its own tokens, a binary search per token; the first workgroup also
+// writes the per-request outputs.  A new page's first slot belongs to a token of
+// the call, so that token's thread writes the table entry, and no thread reads an
+// entry that another one writes.  The sums saturate in 32 unsigned bits, so lengths
+// that no call can hold refuse their requests and wrap nowhere.
+//
+// What bounds it: the latency of one launch and of the chain lengths -> sums ->
+// page -> slot.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "../../include/vdattn.h"
+#include "vd_hw.hpp"
+
+using namespace vd;
+
+namespace {
+
+constexpr int kPageTokens = 16;
+constexpr int kPerThread = 4;  // requests a thread sums at a time
+
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) {
+  return __builtin_elementwise_add_sat(a, b);
+}
+
+// Saturating inclusive sum over the lanes of a wavefront.
+__device__ __forceinline__ uint32_t wave_scan_sat(uint32_t v) {
+#define VD_STEP(ctrl, rows) \
+  v = add_sat(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false))
+  VD_STEP(0x111, 0xf);  // row_shr:1
+  VD_STEP(0x112, 0xf);  // row_shr:2
+  VD_STEP(0x114, 0xf);  // row_shr:4
+  VD_STEP(0x118, 0xf);  // row_shr:8
+  VD_STEP(0x142, 0xa);  // row_bcast:15
+  VD_STEP(0x143, 0xc);  // row_bcast:31
+#undef VD_STEP
+  return v;
+}
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void map_pages_kernel(vd_page_map a, uint32_t num_free,
+                                                            int tile) {
+  constexpr int kChunk = kPerThread * THREADS, kWaves = THREADS / 64;
+  __shared__ uint32_t l_end[kChunk];  // rows up to and with the request
+  __shared__ int l_cached[kChunk];    // its cached tokens, -1: refused
+  __shared__ int l_delta[kChunk];     // page i of the request is free_pages[i + delta]
+  __shared__ uint32_t w_rows[kWaves], w_need[kWaves];
+  __shared__ int l_used;
+  const int tid = threadIdx.x, lane = __lane_id(), wave = uni(tid >> 6);
+  const bool writer = blockIdx.x == 0;
+  const uint32_t rows = (uint32_t)a.total_q_tokens;
+  const uint32_t t0 = blockIdx.x * (uint32_t)tile;
+  const uint32_t t1 = min(t0 + (uint32_t)tile, rows);
+  uint32_t row0 = 0, need0 = 0;  // sums over the chunks before
+  int used = 0;
+  if (tid == 0) l_used = 0;
+  if (writer && tid == 0) a.cu_q_lens[0] = 0;
+  for (int r0 = 0; r0 < a.num_seqs; r0 += kChunk) {
+    const int count = min(kChunk, a.num_seqs - r0);
+    uint32_t end[kPerThread], taken[kPerThread], need[kPerThread];
+    int cached[kPerThread], len[kPerThread], status[kPerThread];
+    uint32_t sum_r = 0, sum_n = 0;
+#pragma unroll
+    for (int j = 0; j < kPerThread; ++j) {
+      const int i = kPerThread * tid + j;
+      const int s = i < count ? a.q_lens[r0 + i] : 0;
+      cached[j] = i < count ? a.cached_lens[r0 + i] : 0;
+      const int64_t n = (int64_t)cached[j] + max(s, 0);
+      const int64_t pages = (n + kPageTokens - 1) >> 4;
+      status[j] = (s < 0 || cached[j] < 0 || n > INT32_MAX ? 1 : 0) | (pages > a.pt_stride ? 2 : 0);
+      len[j] = (int)n;
+      need[j] = status[j] ? 0 : (uint32_t)pages - ((uint32_t)cached[j] + kPageTokens - 1) / kPageTokens;
+      sum_r = end[j] = add_sat(sum_r, (uint32_t)max(s, 0));
+      sum_n = taken[j] = add_sat(sum_n, need[j]);
+    }
+    const uint32_t in_r = wave_scan_sat(sum_r), in_n = wave_scan_sat(sum_n);
+    if (lane == 63) {
+      w_rows[wave] = in_r;
+      w_need[wave] = in_n;
+    }
+    uint32_t ex_r = __shfl_up(in_r, 1), ex_n = __shfl_up(in_n, 1);
+    if (lane == 0) ex_r = ex_n = 0;
+    __syncthreads();
+    uint32_t all_r = row0, all_n = need0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w == wave) {
+        ex_r = add_sat(ex_r, all_r);
+        ex_n = add_sat(ex_n, all_n);
+      }
+      all_r = add_sat(all_r, w_rows[w]);
+      all_n = add_sat(all_n, w_need[w]);
+    }
+#pragma unroll
+    for (int j = 0; j < kPerThread; ++j) {
+      const int i = kPerThread * tid + j;
+      end[j] = add_sat(ex_r, end[j]);
+      taken[j] = add_sat(ex_n, taken[j]);
+      if (end[j] > rows) status[j] |= 8;
+      if (!(status[j] & 8) && need[j] > 0 && taken[j] > num_free) status[j] |= 4;
+      const bool ok = status[j] == 0;
+      l_end[i] = end[j];
+      l_cached[i] = ok ? cached[j] : -1;
+      l_delta[i] = ok ? (int)(taken[j] - need[j]) - (int)(((uint32_t)cached[j] + kPageTokens - 1) / kPageTokens) : 0;
+      if (ok && need[j] > 0) used = (int)taken[j];
+      if (writer && i < count) {
+        a.cu_q_lens[r0 + i + 1] = (int)min(end[j], (uint32_t)INT32_MAX);
+        a.context_lens[r0 + i] = ok ? len[j] : 0;
+        a.status[r0 + i] = status[j];
+      }
+    }
+    __syncthreads();
+    // this workgroup's tokens of the chunk's requests
+    const uint32_t from = min(max(t0, row0), t1), to = min(t1, all_r);
+    for (uint32_t t = from + tid; t < to; t += THREADS) {
+      int lo = 0, hi = count - 1;  // the first request whose end is past t
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (l_end[mid] > t)
+          hi = mid;
+        else
+          lo = mid + 1;
+      }
+      const int c = l_cached[lo];
+      int64_t slot = -1;
+      if (c >= 0) {
+        const int p = c + (int)(t - (lo > 0 ? l_end[lo - 1] : row0));
+        const int i = p / kPageTokens;
+        int32_t* entry = a.page_table + (int64_t)(r0 + lo) * a.pt_stride + i;
+        int page;
+        if (i >= (int)(((uint32_t)c + kPageTokens - 1) / kPageTokens)) {
+          page = a.free_pages[i + l_delta[lo]];
+          if (p % kPageTokens == 0) *entry = page;
+        } else {
+          page = *entry;
+        }
+        if (page >= 0 && page < a.num_pages) slot = (int64_t)page * kPageTokens + p % kPageTokens;
+      }
+      a.slot_mapping[t] = slot;
+    }
+    __syncthreads();  // the next chunk overwrites the arrays
+    row0 = all_r;
+    need0 = all_n;
+  }
+  // rows behind the last request
+  for (uint32_t t = min(max(t0, row0), t1) + tid; t < t1; t += THREADS) a.slot_mapping[t] = -1;
+  if (writer) {
+    if (a.num_seqs == 0) __syncthreads();
+    if (used > 0) atomicMax(&l_used, used);
+    __syncthreads();
+    if (tid == 0) *a.pages_used = l_used;
+  }
+}
+
+}  // namespace
+
+extern "C" int vd_map_pages(const vd_page_map* m, hipStream_t stream) {
+  if (!m || m->num_seqs < 0 || m->total_q_tokens < 0 || m->total_q_tokens > INT32_MAX - 4096 ||
+      m->num_free < 0 || m->num_pages < 0)
+    return VD_ERR_INVALID_ARG;
+  const auto bad = [](const void* p, bool needed, int n) {
+    return (needed && !p) || (uintptr_t)p % n != 0;
+  };
+  const bool any = m->num_seqs > 0;
+  if (bad(m->q_lens, any, 4) || bad(m->cached_lens, any, 4) || bad(m->page_table, any, 4) ||
+      bad(m->context_lens, any, 4) || bad(m->status, any, 4) || (any && m->pt_stride < 1) ||
+      bad(m->free_pages, m->num_free > 0, 4) || bad(m->slot_mapping, m->total_q_tokens > 0, 8) ||
+      bad(m->cu_q_lens, true, 4) || bad(m->pages_used, true, 4))
+    return VD_ERR_INVALID_ARG;
+  // the outputs are written while other workgroups read the lengths
+  if (any && (m->context_lens == m->cached_lens || m->context_lens == m->q_lens ||
+              m->status == m->cached_lens || m->status == m->q_lens))
+    return VD_ERR_INVALID_ARG;
+  const uint32_t num_free = (uint32_t)std::min<int64_t>(m->num_free, INT32_MAX);
+  constexpr int kTile = 1024;  // tokens of a workgroup
+  const unsigned blocks = (unsigned)std::max<int64_t>(1, (m->total_q_tokens + kTile - 1) / kTile);
+  if (m->num_seqs <= 256 * kPerThread)
+    hipLaunchKernelGGL(map_pages_kernel<256>, dim3(blocks), dim3(256), 0, stream, *m, num_free, kTile);
+  else
+    hipLaunchKernelGGL(map_pages_kernel<1024>, dim3(blocks), dim3(1024), 0, stream, *m, num_free, kTile);
+  return hipGetLastError() == hipSuccess ? VD_OK : VD_ERR_LAUNCH;
+}

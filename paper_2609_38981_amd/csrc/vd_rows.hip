@@ -1,0 +1,304 @@
+// vd_rows.hip -- the row operators between the linear layers of libvdattn.so
+// (gfx950): the RMS norm with the residual's addition, and rows in 8 bits with a
+// scale for each 128 values.
+//
+//   norm:  h = bf16_RNE(x + r) (h = x without a residual)
+//          y = (h * (1 / sqrt(sum_k h_k^2 / K + eps))) * w, in fp32
+//          out = bf16_RNE(y), or y in 8 bits
+//   8 bits: of each 128 values of a row (the last group may be shorter)
+//          s = max(max |y|, 2^-117) * fl(1 / 448), code = e4m3_RNE(y * (1 / s))
+//   rows:  y = x, or silu(g) * x = g / (1 + exp(-g)) * x, in 8 bits
+// h is rounded once, before the norm, so a row normed together with its addition
+// has the bits of one normed afterwards; y is rounded once, to the output.  448 is
+// the largest e4m3 value; 2^-117 keeps s and 1 / s normal numbers (an all-zero
+// group: s about 2^-126, codes 0).  A group that holds a NaN has the scale NaN, one
+// that holds an infinity the scale infinity and codes 0 or NaN: every value that
+// such codes stand for is NaN.
+//
+// Row invariance: the sum of a row's squares is one fixed tree -- a lane's values
+// in ascending order, the 16 lanes of a row by halving rotations, the 4 rows, the
+// wavefronts in ascending order -- whose shape follows K alone, and a group's
+// maximum is exact.
+//
+// What bounds them: HBM with many rows, the launch and one chain of load, sum and
+// store with few.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/vdattn.h"
+#include "vd_cas.hpp"
+#include "vd_hw.hpp"
+
+using namespace vd;
+
+namespace {
+
+constexpr int kGroup = 128;       // values per scale
+constexpr int kMaxNormK = 32768;  // 1024 threads of 4 vectors of 8
+constexpr float kMinTop = 0x1p-117f;
+constexpr float kPer448 = 1.0f / 448.0f;
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float bf16_f32(uint16_t b) {
+  return __builtin_bit_cast(float, (uint32_t)b << 16);
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
+}
+
+// Sum (maximum) over the 16 lanes of a row, in all of them, by rotations of 8,
+// 4, 2 and 1: the same operands meet in every lane.
+__device__ __forceinline__ float row_sum(float v) {
+  v += __builtin_bit_cast(float, dpp<0x128>(__builtin_bit_cast(uint32_t, v)));
+  v += __builtin_bit_cast(float, dpp<0x124>(__builtin_bit_cast(uint32_t, v)));
+  v += __builtin_bit_cast(float, dpp<0x122>(__builtin_bit_cast(uint32_t, v)));
+  v += __builtin_bit_cast(float, dpp<0x121>(__builtin_bit_cast(uint32_t, v)));
+  return v;
+}
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  v = max(v, dpp<0x128>(v));
+  v = max(v, dpp<0x124>(v));
+  v = max(v, dpp<0x122>(v));
+  return max(v, dpp<0x121>(v));
+}
+
+// The 8 values of this lane in 8 bits; the 16 lanes of a row hold a group.  All
+// lanes are active; those past the row's end hold zeros.  The maximum is taken of
+// the magnitudes' bits, whose order is the values', infinity and NaN on top.
+__device__ __forceinline__ u32x2 to_codes(const float (&y)[8], float& scale) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __builtin_bit_cast(uint32_t, y[i]) & 0x7FFFFFFFu);
+  top = max(row_max(top), __builtin_bit_cast(uint32_t, kMinTop));
+  scale = __builtin_bit_cast(float, top) * kPer448;
+  const float inv = 1.0f / scale;
+  u32x2 q;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int d = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i] * inv, y[4 * i + 1] * inv, 0, false);
+    q[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2] * inv, y[4 * i + 3] * inv, d, true);
+  }
+  return q;
+}
+
+struct NormArgs {
+  const uint16_t *x, *res, *w;
+  uint16_t* sum;
+  void* out;     // bf16 or e4m3
+  float* scales;
+  int64_t ldx, ldr, lds, ldo, s_row, s_blk, M;
+  int K;
+  float eps;
+};
+
+// A workgroup per row (rows strided by the grid), V vectors of 8 values a lane:
+// vector v of thread t holds values 8 (v T + t) .. + 7 of T threads.
+template <int V, bool RES, bool FP8>
+__global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
+  __shared__ float part[2][16];
+  const int tid = threadIdx.x, lane = __lane_id(), wave = uni(tid >> 6);
+  const int threads = blockDim.x, waves = threads >> 6;
+  const int vecs = a.K / 8;
+  int parity = 0;
+  for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x, parity ^= 1) {
+    float h[V][8];
+    float ss = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int i = v * threads + tid;
+      u16x8 xv = {}, rv = {};
+      if (i < vecs) {
+        xv = *reinterpret_cast<const u16x8*>(a.x + row * a.ldx + 8 * i);
+        if (RES) rv = *reinterpret_cast<const u16x8*>(a.res + row * a.ldr + 8 * i);
+      }
+      u16x8 hv;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        hv[e] = RES ? bf16_rne(bf16_f32(xv[e]) + bf16_f32(rv[e])) : xv[e];
+        h[v][e] = bf16_f32(hv[e]);
+        ss = __builtin_fmaf(h[v][e], h[v][e], ss);
+      }
+      if (RES && i < vecs) *reinterpret_cast<u16x8*>(a.sum + row * a.lds + 8 * i) = hv;
+    }
+    ss = column_sum(row_sum(ss));
+    if (waves > 1) {
+      if (lane == 0) part[parity][wave] = ss;
+      __syncthreads();
+      ss = part[parity][0];
+      for (int w = 1; w < waves; ++w) ss += part[parity][w];
+    }
+    const float r = 1.0f / __builtin_sqrtf(ss / (float)a.K + a.eps);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int i = v * threads + tid;
+      u16x8 wv = {};
+      if (i < vecs) wv = *reinterpret_cast<const u16x8*>(a.w + 8 * i);
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = h[v][e] * r * bf16_f32(wv[e]);
+      if constexpr (FP8) {
+        float scale;
+        if (i >= vecs) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = 0.0f;  // (r may be a NaN)
+        }
+        const u32x2 q = to_codes(y, scale);
+        if (i < vecs) {
+          *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.out) + row * a.ldo + 8 * i) = q;
+          if (i % 16 == 0) a.scales[row * a.s_row + i / 16 * a.s_blk] = scale;
+        }
+      } else if (i < vecs) {
+        u16x8 o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = bf16_rne(y[e]);
+        *reinterpret_cast<u16x8*>(static_cast<uint16_t*>(a.out) + row * a.ldo + 8 * i) = o;
+      }
+    }
+  }
+}
+
+struct RowArgs {
+  const uint16_t *x, *gate;
+  uint8_t* out;
+  float* scales;
+  int64_t ldx, ldg, ldo, s_row, s_blk, groups;
+  int K, per_row;  // values and groups of a row
+};
+
+// 16 lanes per group of 128 values, groups in row order.
+template <bool GATE>
+__global__ __launch_bounds__(256) void quantize_kernel(RowArgs a) {
+  const int lane16 = threadIdx.x & 15;
+  for (int64_t u0 = (int64_t)blockIdx.x * 16; u0 < a.groups; u0 += (int64_t)gridDim.x * 16) {
+    const int64_t u = u0 + (threadIdx.x >> 4);
+    const int64_t row = u / a.per_row;
+    const int g = (int)(u - row * a.per_row);
+    const int k = g * kGroup + 8 * lane16;
+    const bool in = u < a.groups && k < a.K;
+    u16x8 xv = {}, gv = {};
+    if (in) {
+      xv = *reinterpret_cast<const u16x8*>(a.x + row * a.ldx + k);
+      if (GATE) gv = *reinterpret_cast<const u16x8*>(a.gate + row * a.ldg + k);
+    }
+    float y[8], scale;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      y[e] = bf16_f32(xv[e]);
+      if (GATE) {
+        const float s = bf16_f32(gv[e]);
+        y[e] = s / (1.0f + expf(-s)) * y[e];
+      }
+    }
+    const u32x2 q = to_codes(y, scale);
+    if (in) {
+      *reinterpret_cast<u32x2*>(a.out + row * a.ldo + k) = q;
+      if (lane16 == 0) a.scales[row * a.s_row + g * a.s_blk] = scale;
+    }
+  }
+}
+
+bool misaligned(const void* p, int n) { return (uintptr_t)p % n != 0; }
+
+// Rows of 16-bit values that are read or written with 16-byte accesses.
+bool bad_rows(const void* p, int64_t ld, int K) {
+  return !p || misaligned(p, 16) || ld < K || ld % 8 != 0;
+}
+
+// The 8-bit output: rows written 8 bytes at a time, and a scale per group.
+bool bad_codes(const void* q, int64_t ld, const void* s, int64_t s_row, int64_t s_blk, int64_t M,
+               int K) {
+  return !q || misaligned(q, 8) || ld < K || ld % 8 != 0 || !s || misaligned(s, 4) ||
+         (M > 1 && s_row < 1) || (K > kGroup && s_blk < 1);
+}
+
+int check_norm(const NormArgs& a, int64_t K) {
+  if (a.M < 0 || K < 0 || !(a.eps >= 0.0f) || std::isinf(a.eps)) return VD_ERR_INVALID_ARG;
+  if (K % 8 != 0 || K > kMaxNormK) return VD_ERR_UNSUPPORTED;
+  if (a.M == 0 || K == 0) return VD_OK;
+  if (bad_rows(a.x, a.ldx, a.K) || !a.w || misaligned(a.w, 16)) return VD_ERR_INVALID_ARG;
+  if (!a.res != !a.sum) return VD_ERR_INVALID_ARG;
+  if (a.res && (bad_rows(a.res, a.ldr, a.K) || bad_rows(a.sum, a.lds, a.K))) return VD_ERR_INVALID_ARG;
+  return VD_OK;
+}
+
+template <bool FP8>
+int launch_norm(const NormArgs& a, hipStream_t stream) {
+  // 2 vectors a lane (1 for rows of one wavefront's vectors, 4 for rows of more
+  // than 16 wavefronts' pairs): by K alone, the sum's order is its
+  const int per_lane = a.K <= 512 ? 1 : a.K <= 16384 ? 2 : 4;
+  const int waves = (a.K + 512 * per_lane - 1) / (512 * per_lane);
+  const dim3 block(64 * waves);
+  const dim3 grid((unsigned)std::min<int64_t>(a.M, 1 << 16));
+#define VD_NORM(V)                                                                        \
+  if (a.res)                                                                              \
+    hipLaunchKernelGGL((norm_kernel<V, true, FP8>), grid, block, 0, stream, a);           \
+  else                                                                                    \
+    hipLaunchKernelGGL((norm_kernel<V, false, FP8>), grid, block, 0, stream, a)
+  if (per_lane == 1) {
+    VD_NORM(1);
+  } else if (per_lane == 2) {
+    VD_NORM(2);
+  } else {
+    VD_NORM(4);
+  }
+#undef VD_NORM
+  return hipGetLastError() == hipSuccess ? VD_OK : VD_ERR_LAUNCH;
+}
+
+}  // namespace
+
+extern "C" {
+
+int vd_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
+               float eps, void* sum, int64_t lds, void* out, int64_t ldo, int64_t M, int32_t K,
+               hipStream_t stream) {
+  const NormArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(residual),
+                   static_cast<const uint16_t*>(weight), static_cast<uint16_t*>(sum), out, nullptr,
+                   ldx, ldr, lds, ldo, 0, 0, M, K, eps};
+  const int rc = check_norm(a, K);
+  if (rc != VD_OK || M == 0 || K == 0) return rc;
+  if (bad_rows(out, ldo, K)) return VD_ERR_INVALID_ARG;
+  return launch_norm<false>(a, stream);
+}
+
+int vd_rmsnorm_fp8(const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                   const void* weight, float eps, void* sum, int64_t lds, void* out, int64_t ldo,
+                   float* scales, int64_t s_row, int64_t s_blk, int64_t M, int32_t K,
+                   hipStream_t stream) {
+  const NormArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(residual),
+                   static_cast<const uint16_t*>(weight), static_cast<uint16_t*>(sum), out, scales,
+                   ldx, ldr, lds, ldo, s_row, s_blk, M, K, eps};
+  const int rc = check_norm(a, K);
+  if (rc != VD_OK || M == 0 || K == 0) return rc;
+  if (bad_codes(out, ldo, scales, s_row, s_blk, M, K)) return VD_ERR_INVALID_ARG;
+  return launch_norm<true>(a, stream);
+}
+
+int vd_quantize_fp8(const void* x, int64_t ldx, const void* gate, int64_t ldg, void* out,
+                    int64_t ldo, float* scales, int64_t s_row, int64_t s_blk, int64_t M, int32_t K,
+                    hipStream_t stream) {
+  if (M < 0 || K < 0) return VD_ERR_INVALID_ARG;
+  if (K % 8 != 0) return VD_ERR_UNSUPPORTED;
+  if (M == 0 || K == 0) return VD_OK;
+  const int per_row = (K - 1) / kGroup + 1;
+  if (bad_rows(x, ldx, K) || (gate && bad_rows(gate, ldg, K)) ||
+      bad_codes(out, ldo, scales, s_row, s_blk, M, K) || M > INT64_MAX / 2 / per_row)
+    return VD_ERR_INVALID_ARG;
+  const RowArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(gate),
+                  static_cast<uint8_t*>(out), scales, ldx, ldg, ldo, s_row, s_blk, M * per_row, K,
+                  per_row};
+  const dim3 grid((unsigned)std::min<int64_t>((a.groups + 15) / 16, 1 << 20));
+  if (gate)
+    hipLaunchKernelGGL(quantize_kernel<true>, grid, dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL(quantize_kernel<false>, grid, dim3(256), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? VD_OK : VD_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -58,6 +58,16 @@ class _Batch(ctypes.Structure):
                 ("shared_pages", ctypes.c_int32), ("lse", ctypes.c_void_p)]
 
 
+class _PageMap(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("total_q_tokens", ctypes.c_int64),
+                ("q_lens", ctypes.c_void_p), ("cached_lens", ctypes.c_void_p),
+                ("free_pages", ctypes.c_void_p), ("num_free", ctypes.c_int64),
+                ("num_pages", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+                ("pt_stride", ctypes.c_int32), ("cu_q_lens", ctypes.c_void_p),
+                ("context_lens", ctypes.c_void_p), ("slot_mapping", ctypes.c_void_p),
+                ("status", ctypes.c_void_p), ("pages_used", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -71,6 +81,7 @@ def load_library(path: str = LIB_PATH):
                            "python -m paper_2609_38981_amd.build" % path)
     lib = ctypes.CDLL(path)
     P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    F32 = ctypes.c_float
     sig = {
         "vd_attn_create": (ctypes.c_int, [ctypes.POINTER(_Desc), ctypes.POINTER(P)]),
         "vd_attn_destroy": (None, [P]),
@@ -89,6 +100,13 @@ def load_library(path: str = LIB_PATH):
         "vd_attn_validate": (ctypes.c_int, [P, ctypes.POINTER(_Batch), P, P]),
         "vd_kv_write": (ctypes.c_int, [P, P, P, P, I64, P, P, I64, P]),
         "vd_linear": (ctypes.c_int, [P, I64, P, I64, P, I64, I64, I32, I32, P]),
+        "vd_linear_fp8": (ctypes.c_int, [P, I64, P, I64, I64, P, I64, P, I64, I64, P, I64, I64, I32,
+                                         I32, P]),
+        "vd_rmsnorm": (ctypes.c_int, [P, I64, P, I64, P, F32, P, I64, P, I64, I64, I32, P]),
+        "vd_rmsnorm_fp8": (ctypes.c_int, [P, I64, P, I64, P, F32, P, I64, P, I64, P, I64, I64, I64,
+                                          I32, P]),
+        "vd_quantize_fp8": (ctypes.c_int, [P, I64, P, I64, P, I64, P, I64, I64, I64, I32, P]),
+        "vd_map_pages": (ctypes.c_int, [ctypes.POINTER(_PageMap), P]),
         "vd_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "vd_attn_tiling": (ctypes.c_int, [P, ctypes.POINTER(I32), ctypes.POINTER(I32),
                                           ctypes.POINTER(I32)]),
@@ -105,7 +123,7 @@ def declared_functions(header: str = HEADER):
     """Names of the functions include/vdattn.h declares."""
     text = open(header).read()
     text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
-    return sorted(set(re.findall(r"\b(vd_[a-z_]+)\s*\(", text)))
+    return sorted(set(re.findall(r"\b(vd_[a-z0-9_]+)\s*\(", text)))
 
 
 def status_string(status: int) -> str:
@@ -417,4 +435,220 @@ def linear(a: torch.Tensor, b: torch.Tensor, out: Optional[torch.Tensor] = None,
         raise ValueError("out must be bf16 [M, N] with contiguous rows")
     _check(lib.vd_linear(a.data_ptr(), a.stride(0), b.data_ptr(), b.stride(0), out.data_ptr(),
                          out.stride(0), M, N, K, _stream(stream)), "vd_linear")
+    return out
+
+
+# ---------------------------------------------------------------------------
+# The operators around the attention: 8-bit rows and weights, the norm, the page map
+# ---------------------------------------------------------------------------
+E4M3 = torch.float8_e4m3fn
+SCALE_BLOCK = 128  # values per scale
+
+
+def _call(fn, what: str, args, t: torch.Tensor, stream):
+    """One C call on t's device (the library launches on the current one), on ``stream``
+    or that device's current stream."""
+    index = t.device.index
+    if index == torch.cuda.current_device():
+        rc = fn(*args, _stream(stream))
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, _stream(stream))
+    if rc != VD_OK:
+        raise VdError(rc, what)
+
+
+def _rows(t, name: str, dtype, device=None, shape=None):
+    """A 2-D device tensor whose rows are contiguous (they may be strided)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
+        raise TypeError("%s must be a %s device tensor" % (name, dtype))
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError("%s must be 2-D with contiguous rows" % name)
+    if device is not None and t.device != device:
+        raise ValueError("%s must be on %s" % (name, device))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+
+
+def _ld(t: torch.Tensor) -> int:
+    """The row stride; a single row has none of its own."""
+    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 15) // 16 * 16
+
+
+def _scales(s, name: str, rows: int, K: int, device):
+    """fp32 scales [rows, ceil(K / 128)] of any strides."""
+    if not isinstance(s, torch.Tensor) or not s.is_cuda or s.dtype != torch.float32:
+        raise TypeError("%s must be a float32 device tensor" % name)
+    if s.dim() != 2 or s.shape[0] != rows or s.shape[1] != -(-K // SCALE_BLOCK):
+        raise ValueError("%s must be [%d, %d], got %s" % (name, rows, -(-K // SCALE_BLOCK),
+                                                          tuple(s.shape)))
+    if s.device != device:
+        raise ValueError("%s must be on %s" % (name, device))
+
+
+def _new_codes(M: int, K: int, device, out, scales):
+    """The 8-bit output of an M x K result: codes, and scales that lie side by side for
+    each block of K (what linear_fp8 reads fastest)."""
+    if out is None:
+        out = torch.empty((M, K), dtype=E4M3, device=device)
+    else:
+        _rows(out, "out", E4M3, device, (M, K))
+    if scales is None:
+        scales = torch.empty((-(-K // SCALE_BLOCK), M), dtype=torch.float32, device=device).t()
+    else:
+        _scales(scales, "scales", M, K, device)
+    return out, scales
+
+
+def _scale_strides(s: torch.Tensor):
+    return tuple(s.stride(i) if s.shape[i] > 1 else 1 for i in (0, 1))
+
+
+def linear_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
+               out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Batch-invariant linear layer on 8-bit matrices (vd_linear_fp8): a [M, K] e4m3 with
+    scales [M, ceil(K / 128)], b [N, K] e4m3 with scales [ceil(N / 128), ceil(K / 128)], out
+    [M, N] bf16.  Rows may be strided; the scales may have any strides."""
+    lib = load_library()
+    _rows(a, "a", E4M3)
+    _rows(b, "b", E4M3, a.device)
+    M, K = a.shape
+    N = b.shape[0]
+    if b.shape[1] != K:
+        raise ValueError("a is [M, %d] but b is [N, %d]" % (K, b.shape[1]))
+    _scales(a_scales, "a_scales", M, K, a.device)
+    _scales(b_scales, "b_scales", -(-N // SCALE_BLOCK), K, a.device)
+    if out is None:
+        out = torch.empty((M, N), dtype=torch.bfloat16, device=a.device)
+    else:
+        _rows(out, "out", torch.bfloat16, a.device, (M, N))
+    _call(lib.vd_linear_fp8, "vd_linear_fp8",
+          (a.data_ptr(), _ld(a), a_scales.data_ptr(), a_scales.stride(0), a_scales.stride(1),
+           b.data_ptr(), _ld(b), b_scales.data_ptr(), b_scales.stride(0), b_scales.stride(1),
+           out.data_ptr(), _ld(out) if M > 1 else N, M, N, K), a, stream)
+    return out
+
+
+def _norm_inputs(x, weight, residual, residual_out):
+    _rows(x, "x", torch.bfloat16)
+    M, K = x.shape
+    if not isinstance(weight, torch.Tensor) or weight.dtype != torch.bfloat16 or not weight.is_cuda:
+        raise TypeError("weight must be a bf16 device tensor")
+    if weight.shape != (K,) or not weight.is_contiguous() or weight.device != x.device:
+        raise ValueError("weight must be [%d], contiguous, on %s" % (K, x.device))
+    if residual is None:
+        if residual_out is not None:
+            raise ValueError("residual_out needs a residual")
+        return (None, 0), (None, 0), None
+    _rows(residual, "residual", torch.bfloat16, x.device, x.shape)
+    if residual_out is None:
+        residual_out = torch.empty((M, K), dtype=torch.bfloat16, device=x.device)
+    else:
+        _rows(residual_out, "residual_out", torch.bfloat16, x.device, x.shape)
+    return ((residual.data_ptr(), _ld(residual)), (residual_out.data_ptr(), _ld(residual_out)),
+            residual_out)
+
+
+def rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5,
+            residual: Optional[torch.Tensor] = None, residual_out: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None, stream=None):
+    """RMS norm of the rows of x [M, K] (vd_rmsnorm), bf16.  With a residual the rows of
+    x + residual are normed, and (out, x + residual) is returned; ``residual_out`` may be x or
+    the residual.  Rows may be strided."""
+    lib = load_library()
+    (r, ldr), (s, lds), residual_out = _norm_inputs(x, weight, residual, residual_out)
+    M, K = x.shape
+    if out is None:
+        out = torch.empty((M, K), dtype=torch.bfloat16, device=x.device)
+    else:
+        _rows(out, "out", torch.bfloat16, x.device, x.shape)
+    _call(lib.vd_rmsnorm, "vd_rmsnorm", (x.data_ptr(), _ld(x), r, ldr, weight.data_ptr(), eps, s, lds,
+                                         out.data_ptr(), _ld(out), M, K), x, stream)
+    return out if residual is None else (out, residual_out)
+
+
+def rmsnorm_fp8(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5,
+                residual: Optional[torch.Tensor] = None,
+                residual_out: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                scales: Optional[torch.Tensor] = None, stream=None):
+    """rmsnorm with its result in 8 bits (vd_rmsnorm_fp8): (codes [M, K] e4m3, scales
+    [M, ceil(K / 128)]), with a residual (codes, scales, x + residual)."""
+    lib = load_library()
+    (r, ldr), (s, lds), residual_out = _norm_inputs(x, weight, residual, residual_out)
+    M, K = x.shape
+    out, scales = _new_codes(M, K, x.device, out, scales)
+    _call(lib.vd_rmsnorm_fp8, "vd_rmsnorm_fp8",
+          (x.data_ptr(), _ld(x), r, ldr, weight.data_ptr(), eps, s, lds, out.data_ptr(), _ld(out),
+           scales.data_ptr(), *_scale_strides(scales), M, K), x, stream)
+    return (out, scales) if residual is None else (out, scales, residual_out)
+
+
+def quantize_fp8(x: torch.Tensor, gate: Optional[torch.Tensor] = None,
+                 out: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                 stream=None):
+    """The rows of x [M, K] bf16 in 8 bits (vd_quantize_fp8): (codes [M, K] e4m3, scales
+    [M, ceil(K / 128)]).  With a gate [M, K], those of silu(gate) * x.  Rows may be strided."""
+    lib = load_library()
+    _rows(x, "x", torch.bfloat16)
+    M, K = x.shape
+    if gate is not None:
+        _rows(gate, "gate", torch.bfloat16, x.device, x.shape)
+    out, scales = _new_codes(M, K, x.device, out, scales)
+    _call(lib.vd_quantize_fp8, "vd_quantize_fp8",
+          (x.data_ptr(), _ld(x), _ptr(gate), 0 if gate is None else _ld(gate), out.data_ptr(),
+           _ld(out), scales.data_ptr(), *_scale_strides(scales), M, K), x, stream)
+    return out, scales
+
+
+@dataclass
+class PageMap:
+    """What map_pages makes of one call's lengths (device tensors)."""
+    cu_q_lens: torch.Tensor     # [B + 1] int32
+    context_lens: torch.Tensor  # [B] int32, 0: refused
+    slot_mapping: torch.Tensor  # [total_q_tokens] int64, -1: no slot
+    status: torch.Tensor        # [B] int32 bit masks, 0: fine
+    pages_used: torch.Tensor    # [1] int32, taken from the free list's start
+
+
+def map_pages(q_lens: torch.Tensor, cached_lens: torch.Tensor, free_pages: torch.Tensor,
+              page_table: torch.Tensor, num_pages: int, total_q_tokens: int,
+              out: Optional[PageMap] = None, stream=None) -> PageMap:
+    """The page map of one call (vd_map_pages): from the new and cached tokens of every
+    request (int32 [B]) the query offsets, context lengths and slots of its tokens; the pages
+    that the new tokens need are taken from ``free_pages`` (int32) and written into
+    ``page_table`` (int32 [B, stride], in place).  ``total_q_tokens`` rows of slots, the ones
+    behind the last request -1."""
+    lib = load_library()
+    for t, name in ((q_lens, "q_lens"), (cached_lens, "cached_lens"), (free_pages, "free_pages"),
+                    (page_table, "page_table")):
+        _need(t, name, torch.int32)
+    B, T = q_lens.numel(), int(total_q_tokens)
+    if q_lens.dim() != 1 or cached_lens.shape != q_lens.shape:
+        raise ValueError("q_lens and cached_lens must be [num_seqs]")
+    if page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError("page_table must be [num_seqs, stride]")
+    dev = page_table.device
+    if out is None:
+        i32 = torch.empty(3 * B + 2, dtype=torch.int32, device=dev)
+        out = PageMap(i32[:B + 1], i32[B + 1:2 * B + 1],
+                      torch.empty(max(T, 0), dtype=torch.int64, device=dev),
+                      i32[2 * B + 1:3 * B + 1], i32[3 * B + 1:])
+    else:
+        for t, name, dtype, n in ((out.cu_q_lens, "cu_q_lens", torch.int32, B + 1),
+                                  (out.context_lens, "context_lens", torch.int32, B),
+                                  (out.slot_mapping, "slot_mapping", torch.int64, T),
+                                  (out.status, "status", torch.int32, B),
+                                  (out.pages_used, "pages_used", torch.int32, 1)):
+            _need(t, name, dtype, n)
+            if t.device != dev:
+                raise ValueError("%s must be on %s" % (name, dev))
+    for t, name in ((q_lens, "q_lens"), (cached_lens, "cached_lens"), (free_pages, "free_pages")):
+        if t.device != dev:
+            raise ValueError("%s must be on %s" % (name, dev))
+    m = _PageMap(B, T, q_lens.data_ptr(), cached_lens.data_ptr(), free_pages.data_ptr(),
+                 free_pages.numel(), int(num_pages), page_table.data_ptr(),
+                 page_table.shape[1] if B else 1, out.cu_q_lens.data_ptr(),
+                 out.context_lens.data_ptr(), out.slot_mapping.data_ptr(), out.status.data_ptr(),
+                 out.pages_used.data_ptr())
+    _call(lib.vd_map_pages, "vd_map_pages", (ctypes.byref(m),), page_table, stream)
     return out
