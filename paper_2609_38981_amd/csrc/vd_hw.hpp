@@ -37,7 +37,20 @@ __device__ __forceinline__ void lds_dma16(const void* src, uint32_t m0val) {
       : "memory");
 }
 
-// The same of 4 bytes per lane: lane l's land at LDS byte address m0val + 4 l.
+// The same with the source as a uniform base and a 32-bit offset per lane, and of 4
+// bytes per lane (lane l's land at LDS byte address m0val + 4 l).
+__device__ __forceinline__ void lds_dma16_at(const void* base, uint32_t off, uint32_t m0val) {
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %3\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %1\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "s"(base), "v"(off), "s"(m0val)
+      : "memory");
+}
 __device__ __forceinline__ void lds_dma4(const void* src, uint32_t m0val) {
   uint32_t saved;
   asm volatile(

@@ -27,6 +27,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/vdattn.h"
 #include "vd_cas.hpp"
@@ -37,7 +38,9 @@ using namespace vd;
 namespace {
 
 constexpr int kBlock = 128;  // values of K per scale (one byte each)
+constexpr int kLast = 2;     // rows of tiles of a step taken together at its end
 constexpr int kGroupM = 4;   // row tiles per group of the tile order
+constexpr int64_t kMaxStride = INT64_C(1) << 29;  // 7 rows within 32 bits of a copy's first one
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -84,17 +87,24 @@ struct Tile {
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
 };
 
-// Waits until at most `later` stages of N copies each are outstanding.
-template <int N, int MAX>
-__device__ __forceinline__ void wait_stages(int later) {
-  if constexpr (MAX == 0) {
-    wait_vmcnt<0>();
-  } else {
-    if (later >= MAX)
-      wait_vmcnt<N * MAX>();
-    else
-      wait_stages<N, MAX - 1>(later);
-  }
+// Tile order: groups of kGroupM row tiles, each sweeping the column tiles (row tile
+// fastest); XCD x takes the x-th contiguous share of the order, so that the
+// panels of a die's workgroups meet in its L2.  False: no tile for this workgroup.
+__device__ __forceinline__ bool tile_of(uint32_t block, int tiles_m, int tiles_n, int xcd_shift,
+                                        int bm, int bn, int64_t& m0, int& n0) {
+  const int64_t total = (int64_t)tiles_m * tiles_n;
+  const int xcds = 1 << xcd_shift;
+  const int64_t per_xcd = (total + xcds - 1) >> xcd_shift;
+  const int64_t jx = block >> xcd_shift;
+  const int64_t i = (int64_t)(block & (xcds - 1)) * per_xcd + jx;
+  if (jx >= per_xcd || i >= total) return false;
+  const int64_t group = i / ((int64_t)kGroupM * tiles_n);
+  const int64_t first_m = group * kGroupM;
+  const int size_m = (int)((tiles_m - first_m) < kGroupM ? (tiles_m - first_m) : kGroupM);
+  const int in_group = (int)(i - group * (int64_t)kGroupM * tiles_n);
+  m0 = (first_m + in_group % size_m) * bm;
+  n0 = (in_group / size_m) * bn;
+  return true;
 }
 
 template <class T>
@@ -104,42 +114,29 @@ __global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(T::
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int wave = uni(threadIdx.x >> 6);
   const int lane = __lane_id();
-  // tile order: groups of kGroupM row tiles, each sweeping the column tiles
-  // (row tile fastest); XCD x takes the x-th contiguous share of the order
-  const int64_t total = (int64_t)tiles_m * tiles_n;
-  const int xcds = 1 << xcd_shift;
-  const int64_t per_xcd = (total + xcds - 1) >> xcd_shift;
-  const int64_t jx = blockIdx.x >> xcd_shift;
-  if (jx >= per_xcd) return;
-  const int64_t i = (int64_t)(blockIdx.x & (xcds - 1)) * per_xcd + jx;
-  if (i >= total) return;
-  const int64_t group = i / ((int64_t)kGroupM * tiles_n);
-  const int64_t first_m = group * kGroupM;
-  const int size_m = (int)((tiles_m - first_m) < kGroupM ? (tiles_m - first_m) : kGroupM);
-  const int in_group = (int)(i - group * (int64_t)kGroupM * tiles_n);
-  const int64_t m0 = (first_m + in_group % size_m) * T::BM;
-  const int n0 = (in_group / size_m) * T::BN;
+  int64_t m0;
+  int n0;
+  if (!tile_of(blockIdx.x, tiles_m, tiles_n, xcd_shift, T::BM, T::BN, m0, n0)) return;
 
   // Copies of a block: 1 KB (8 rows of 128 bytes) each, of the A tile and then the
   // B tile; lane l of a copy carries row l / 8 of it and 16-byte slot l % 8, i.e.
   // source chunk slot ^ (row & 7), so that the rows an operand read touches at one
   // chunk lie in distinct banks.  Rows past M (or N) repeat the last row: in
   // bounds, and never stored.
-  const uint8_t* src[T::kTileCopies];
-  int ck[T::kTileCopies];  // the lane's byte within the block
+  const uint8_t* src[T::kTileCopies];  // uniform: the copy's first row
+  uint32_t off[T::kTileCopies];        // the lane's byte from there
+  const uint32_t ck = 16 * ((lane % 8) ^ (lane / 8));
 #pragma unroll
   for (int j = 0; j < T::kTileCopies; ++j) {
     const int u = wave * T::kTileCopies + j;
     const bool is_a = u < T::kCopiesA;
-    const int r = (is_a ? u : u - T::kCopiesA) * 8 + lane / 8;
-    ck[j] = 16 * ((lane % 8) ^ (r & 7));
-    if (is_a) {
-      const int64_t ra = m0 + r < q.M ? m0 + r : q.M - 1;
-      src[j] = q.a + ra * q.lda;
-    } else {
-      const int rb = n0 + r < q.N ? n0 + r : q.N - 1;
-      src[j] = q.b + (int64_t)rb * q.ldb;
-    }
+    const int64_t r0 = is_a ? m0 + 8 * u : n0 + 8 * (u - T::kCopiesA);
+    const int64_t last = (is_a ? q.M : q.N) - 1;
+    const int64_t ld = is_a ? q.lda : q.ldb;
+    const int64_t r = r0 < last ? r0 : last;
+    const int64_t dr = r0 + lane / 8 < last ? lane / 8 : last - r;
+    src[j] = (is_a ? q.a : q.b) + r * ld;
+    off[j] = (uint32_t)(dr * ld) + ck;
   }
   // Scales of a block: wavefront w copies those of rows 64 w .. + 63 of a; the next
   // one those of the tile's 128-row blocks of b; the others repeat that.
@@ -152,26 +149,29 @@ __global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(T::
     scale_step = q.as_blk;
   } else {
     const int last = (q.N - 1) / kBlock;
-    const int nb = n0 / kBlock + lane;
+    const int nb = n0 / kBlock + min(lane, (T::BN - 1) / kBlock);
     scale_src = q.bs + (int64_t)(nb < last ? nb : last) * q.bs_row;
     scale_step = q.bs_blk;
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int steps = (blocks + T::kBlocks - 1) / T::kBlocks;
-  auto fetch = [&](int step) {
-    const uint32_t st = lds0 + (step % ST) * T::kStage;
-#pragma unroll
-    for (int c = 0; c < T::kBlocks; ++c) {
-      // (blocks and chunks past K repeat the last ones, in bounds and never used)
-      const int blk = min(step * T::kBlocks + c, blocks - 1);
-      const uint32_t at = st + c * T::kStageBlock;
-      const bool half = blk * kBlock + kBlock > q.K;
-#pragma unroll
-      for (int j = 0; j < T::kTileCopies; ++j)
-        lds_dma16(src[j] + (int64_t)blk * kBlock + (half ? ck[j] & 63 : ck[j]),
-                  uni((int)(at + 1024 * (wave * T::kTileCopies + j))));
+  // copy j of block c of a step (the last one: scales); blocks and chunks past K
+  // repeat the last ones, in bounds and never used
+  auto fetch_one = [&](int step, int c, int j) {
+    const int blk = min(step * T::kBlocks + c, blocks - 1);
+    const uint32_t at = lds0 + (step % ST) * T::kStage + c * T::kStageBlock;
+    const uint32_t back = blk * kBlock + kBlock > q.K ? ck & 64 : 0;
+    if (j < T::kTileCopies)
+      lds_dma16_at(src[j] + (int64_t)blk * kBlock, off[j] - back,
+                   uni((int)(at + 1024 * (wave * T::kTileCopies + j))));
+    else
       lds_dma4(scale_src + blk * scale_step, uni((int)(at + T::kTileA + T::kTileB + 256 * wave)));
-    }
+  };
+  auto fetch = [&](int step) {
+#pragma unroll
+    for (int c = 0; c < T::kBlocks; ++c)
+#pragma unroll
+      for (int j = 0; j <= T::kTileCopies; ++j) fetch_one(step, c, j);
   };
 
   // this wavefront's part: rows wm .. + 16 XB - 1 of a, wn .. + 16 YB - 1 of b
@@ -184,7 +184,19 @@ __global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(T::
 #pragma unroll
     for (int y = 0; y < YB; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  auto block = [&](const char* st, bool half) {
+  // One block of K.  The fused multiply-adds of a row of tiles are issued between the
+  // matrix steps of the next one, whose weights are read a row ahead: a matrix step
+  // holds the core for 32 cycles, four multiply-adds the vector unit for 16.  The
+  // last row's wait for the next block, behind its operand reads and the copies.
+  f32x4 p[2][XB];
+  float s[XB];
+  auto fold = [&](int y) {
+#pragma unroll
+    for (int x = 0; x < XB; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[x][y][e] = __builtin_fmaf(p[y & 1][x][e], s[x], acc[x][y][e]);
+  };
+  auto block = [&](const char* st, bool half, auto copies) {
     const char* TA = st;
     const char* TB = st + T::kTileA;
     const float* S = reinterpret_cast<const float*>(st + T::kTileA + T::kTileB);
@@ -195,45 +207,73 @@ __global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(T::
       if (half) hi = i32x4{0, 0, 0, 0};
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    const float bs = S[64 * T::kScaleWaves + nb];
-    i32x8 xa[XB];
-    float s[XB];
+    i32x8 xa[XB], wv[2];
+    wv[0] = operand(TB + (wn + col) * kBlock);
 #pragma unroll
-    for (int x = 0; x < XB; ++x) {
-      xa[x] = operand(TA + (wm + 16 * x + col) * kBlock);
-      s[x] = S[wm + 16 * x + col] * bs;
-    }
+    for (int x = 0; x < XB; ++x) xa[x] = operand(TA + (wm + 16 * x + col) * kBlock);
+    const float bs = S[64 * T::kScaleWaves + nb];
+    float ns[XB];
+#pragma unroll
+    for (int x = 0; x < XB; ++x) ns[x] = S[wm + 16 * x + col];
+    __builtin_amdgcn_sched_barrier(0);
+    copies();
+    fold(YB - 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int x = 0; x < XB; ++x) s[x] = ns[x] * bs;
 #pragma unroll
     for (int y = 0; y < YB; ++y) {
-      const i32x8 wv = operand(TB + (wn + 16 * y + col) * kBlock);
+      if (y + 1 < YB) wv[(y + 1) & 1] = operand(TB + (wn + 16 * (y + 1) + col) * kBlock);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = 0; x < XB; ++x) {
-        const f32x4 p = block_product(wv, xa[x]);
+        p[y & 1][x] = block_product(wv[y & 1], xa[x]);
+        if (y > 0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[x][y][e] = __builtin_fmaf(p[e], s[x], acc[x][y][e]);
+          for (int e = 0; e < 4; ++e)
+            acc[x][y - 1][e] = __builtin_fmaf(p[(y - 1) & 1][x][e], s[x], acc[x][y - 1][e]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
 
   // One barrier per step: after it, step t's copies are visible to every
   // wavefront and every wavefront is done with step t - 1, whose stage the
-  // copies of step t + ST - 1 then refill while step t is computed.
+  // copies of step t + ST - 1 then refill while step t is computed.  Those past
+  // the last step repeat its last block and are never read, so every step waits
+  // for the same count.
+  if (steps > 0) {
 #pragma unroll
-  for (int t = 0; t < ST - 1; ++t)
-    if (t < steps) fetch(t);
-  for (int t = 0; t < steps; ++t) {
-    wait_stages<T::kCopies, ST - 2>(steps - 1 - t);
-    lds_barrier();
-    if (t + ST - 1 < steps) fetch(t + ST - 1);
-    const char* st = lds + (t % ST) * T::kStage;
-    if ((t + 1) * T::kBlocks * kBlock <= q.K) {
-#pragma unroll
-      for (int c = 0; c < T::kBlocks; ++c) block(st + c * T::kStageBlock, false);
-    } else {
-      for (int c = 0; t * T::kBlocks + c < blocks; ++c)
-        block(st + c * T::kStageBlock, (t * T::kBlocks + c + 1) * kBlock > q.K);
-    }
+    for (int t = 0; t < ST - 1; ++t) fetch(t);
   }
+  const int full = q.K / T::BK;  // whole steps; the rest of K is one step with less
+  auto begin = [&](int t) {
+    wait_vmcnt<T::kCopies*(ST - 2)>();
+    lds_barrier();
+    return (const char*)lds + (t % ST) * T::kStage;
+  };
+#pragma unroll
+  for (int x = 0; x < XB; ++x) {
+    s[x] = 0.0f;
+    p[(YB - 1) & 1][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  for (int t = 0; t < full; ++t) {
+    const char* st = begin(t);
+#pragma unroll
+    for (int c = 0; c < T::kBlocks; ++c)
+      block(st + c * T::kStageBlock, false, [&] {
+#pragma unroll
+        for (int j = 0; j <= T::kTileCopies; ++j) fetch_one(t + ST - 1, c, j);
+      });
+  }
+  if (full < steps) {
+    const char* st = begin(full);
+    for (int c = 0; full * T::kBlocks + c < blocks; ++c)
+      block(st + c * T::kStageBlock, (full * T::kBlocks + c + 1) * kBlock > q.K, [] {});
+  }
+  wait_vmcnt<0>();
+  fold(YB - 1);
 
   // result e of tile (x, y) in lane (col, grp): row 16 x + col, column 16 y + 4 grp + e
   const bool wide = q.ldc % 4 == 0 && (uintptr_t)q.c % 8 == 0;
@@ -259,6 +299,396 @@ __global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(T::
   }
 }
 
+// ---------------------------------------------------------------------------
+// The kernel for many rows: tiles of WM x WN wavefronts of XB x YB steps each, a
+// block of K per step, two stages of LDS (A0 A1 B0 B1 S0 S1).
+//
+// A step's operand reads, matrix steps, multiply-adds and copies all run beside
+// each other: the activations of step t + 1 are read into registers of their own
+// during the last row of step t, the weights a row ahead, and a row's
+// multiply-adds are issued between the matrix steps of the next row.  The one
+// barrier stands before the last row: there every wavefront has read all of stage
+// t (the copies of t + 2 refill it) and its copies of t + 1, issued a step ago,
+// have landed.
+// ---------------------------------------------------------------------------
+template <int WM_, int WN_, int XB_, int YB_, int ST_, int kPer_>
+struct Wide {
+  static constexpr int kPer = kPer_, ST = ST_;
+  static constexpr int WM = WM_, WN = WN_, XB = XB_, YB = YB_;
+  static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+  static constexpr int BM = WM * 16 * XB, BN = WN * 16 * YB;
+  static constexpr int kTileA = BM * kBlock, kTileB = BN * kBlock, kScales = 256 * kWaves;
+  static constexpr int kStage = kTileA + kTileB + kScales;
+  static constexpr int kLds = ST * kStage;
+  static constexpr int kCopiesA = kTileA / 1024 / kWaves, kCopiesB = kTileB / 1024 / kWaves;
+  static constexpr int kCopies = kCopiesA + kCopiesB;  // per wavefront and step
+  static constexpr int kScaleWaves = (BM + 63) / 64;
+  static_assert(kCopiesA * kWaves * 1024 == kTileA && kCopiesB * kWaves * 1024 == kTileB, "copy split");
+  static_assert(kCopies * kPer < XB * YB, "a step's copies are issued before its barrier");
+  static_assert(kScaleWaves < kWaves, "a wavefront for the weights' scales");
+  static_assert(kBlock % (16 * YB) == 0 && YB % 4 == 0, "a wavefront's columns lie in one block of the weights' scales");
+  static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
+};
+
+template <class T>
+__device__ __forceinline__ void wide_tile(const Call& q, int64_t m0, int n0) {
+  constexpr int XB = T::XB, YB = T::YB, ST = T::ST;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int wave = uni(threadIdx.x >> 6);
+  const int lane = __lane_id();
+  // Copies: as in the kernel above; a wavefront's copy j carries 8 rows of a (j <
+  // kCopiesA) or b.  Rows past the last read the end of the last one's block
+  // instead (limit), in bounds and never stored.
+  const uint8_t* src[T::kCopies];
+  uint32_t limit[T::kCopies];
+#pragma unroll
+  for (int j = 0; j < T::kCopies; ++j) {
+    const bool is_a = j < T::kCopiesA;
+    const int64_t r0 = is_a ? m0 + 8 * (wave * T::kCopiesA + j) : n0 + 8 * (wave * T::kCopiesB + j - T::kCopiesA);
+    const int64_t last = (is_a ? q.M : q.N) - 1, ld = is_a ? q.lda : q.ldb;
+    const int64_t r = r0 < last ? r0 : last;
+    const int64_t below = last - r < 7 ? last - r : 7;
+    src[j] = (is_a ? q.a : q.b) + r * ld;
+    limit[j] = (uint32_t)(below * ld) + 112;
+  }
+  const uint32_t ck = 16 * ((lane % 8) ^ (lane / 8));
+  const uint32_t off_a = (uint32_t)((lane / 8) * q.lda) + ck, off_b = (uint32_t)((lane / 8) * q.ldb) + ck;
+  const int blocks = (q.K + kBlock - 1) / kBlock;
+  const float* scale_src;
+  int64_t scale_step;
+  if (wave < T::kScaleWaves) {
+    const int64_t m = m0 + 64 * wave + lane;
+    scale_src = q.as + (m < q.M ? m : q.M - 1) * q.as_row;
+    scale_step = q.as_blk;
+  } else {
+    // (lanes past the tile's blocks repeat its last one: few lines)
+    const int end = (q.N - 1) / kBlock, at = n0 / kBlock + min(lane, (T::BN - 1) / kBlock);
+    scale_src = q.bs + (int64_t)(at < end ? at : end) * q.bs_row;
+    scale_step = q.bs_blk;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+  const uint32_t dst_a = lds0 + 1024 * T::kCopiesA * wave, dst_b = lds0 + T::kTileA + 1024 * T::kCopiesB * wave;
+  const uint32_t dst_scale = lds0 + T::kTileA + T::kTileB + 256 * wave;
+  // copy j of step t (the last one: scales) into its stage (from byte st on); past K: the
+  // last block again
+  auto fetch = [&](int t, int st, int j) {
+    const int blk = min(t, blocks - 1);
+    if (j < T::kCopies) {
+      // (a half block: its bytes past K are those before it, never used)
+      const bool half = blk * kBlock + kBlock > q.K;
+      const uint32_t off = j < T::kCopiesA ? off_a : off_b;
+      const uint32_t o = half ? off - (ck & 64) : off, lim = half ? limit[j] - 64 : limit[j];
+      const uint32_t at = j < T::kCopiesA ? dst_a + st + 1024 * j
+                                          : dst_b + st + 1024 * (j - T::kCopiesA);
+      lds_dma16_at(src[j] + (int64_t)blk * kBlock, min(o, lim), uni((int)at));
+    } else {
+      lds_dma4(scale_src + blk * scale_step, uni((int)(dst_scale + st)));
+    }
+  };
+
+  const int wm = 16 * XB * (wave / T::WN), wn = 16 * YB * (wave % T::WN);
+  const int col = lane & 15, grp = lane >> 4;
+  const int o0 = (grp ^ (col & 7)) << 4, o1 = ((4 + grp) ^ (col & 7)) << 4;
+  const char* a0 = lds + (wm + col) * kBlock;
+  const char* b0 = lds + T::kTileA + (wn + col) * kBlock;
+  const char* s0 = lds + T::kTileA + T::kTileB + 4 * (wm + col);
+  const char* t0 = lds + T::kTileA + T::kTileB + 4 * (64 * T::kScaleWaves + (n0 + wn) / kBlock - n0 / kBlock);
+  auto operand = [&](const char* base, int at) {
+    const i32x4 lo = *reinterpret_cast<const i32x4*>(base + o0 + at);
+    const i32x4 hi = *reinterpret_cast<const i32x4*>(base + o1 + at);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  // Matrix step i of a block: rows of tiles one after another, but the last kLast rows
+  // together, column by column, so that an activation operand is free after its kLast
+  // steps there and the next block's is read into its registers.  The weights' operands
+  // go through 4 sets of registers.
+  constexpr int kSteps = XB * YB, kFirst = YB - kLast;
+  constexpr auto x_of = [](int i) { return i < XB * kFirst ? i % XB : (i - XB * kFirst) / kLast; };
+  constexpr auto y_of = [](int i) { return i < XB * kFirst ? i / XB : kFirst + (i - XB * kFirst) % kLast; };
+  f32x4 acc[XB][YB], p[4];
+  i32x8 xa[XB], wv[4];
+  float s[XB], ns[XB], bs;
+#pragma unroll
+  for (int x = 0; x < XB; ++x) {
+    s[x] = 0.0f;
+#pragma unroll
+    for (int y = 0; y < YB; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) p[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto fold = [&](int i) {
+    const int x = x_of(i), y = y_of(i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[x][y][e] = __builtin_fmaf(p[i % 4][e], s[x], acc[x][y][e]);
+  };
+  auto read_x = [&](int st, int x) {
+    xa[x] = operand(a0 + st, 16 * x * kBlock);
+    ns[x] = *reinterpret_cast<const float*>(s0 + st + 64 * x);
+  };
+  auto read_w = [&](int st, int y) { wv[y % 4] = operand(b0 + st, 16 * y * kBlock); };
+  auto read_bs = [&](int st) { bs = *reinterpret_cast<const float*>(t0 + st); };
+  // st, next: the stages of this step and of the next one; before: of the step ST - 1 ahead
+  auto step = [&](int t, int st, int next, int before) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int x = x_of(i), y = y_of(i);
+      if (y < kFirst && x == 0) {
+        if (y == 0) {
+#pragma unroll
+          for (int k = 1; k < 4; ++k) read_w(st, k);
+        } else if (y + 3 < YB) {
+          read_w(st, y + 3);
+        }
+      }
+      if (i == XB * kFirst) {
+        wait_vmcnt<(ST - 2) * (T::kCopies + 1)>();
+        lds_barrier();
+        read_w(next, 0);
+        read_bs(next);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      fold((i + kSteps - 4) % kSteps);
+      if (i == 3) {
+#pragma unroll
+        for (int k = 0; k < XB; ++k) s[k] = ns[k] * bs;
+      }
+      p[i % 4] = block_product(wv[y % 4], xa[x]);
+      if (y + 1 == YB) read_x(next, x);
+#pragma unroll
+      for (int j = 0; j <= T::kCopies; ++j) {
+        // copies of t + ST into this stage from the barrier on, one every kPer matrix
+        // steps, the last of them in the next block (into the stage before it)
+        const int at = XB * kFirst + j * T::kPer;
+        if (at == i) fetch(t + ST, st, j);
+        if (at - kSteps == i) fetch(t + ST - 1, before, j);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  if (blocks > 0) {
+    constexpr int in_step = (kSteps - XB * kFirst - 1) / T::kPer + 1;  // copies of a step issued within it
+    constexpr int early = in_step < T::kCopies + 1 ? in_step : T::kCopies + 1;
+#pragma unroll
+    for (int t = 0; t < ST; ++t)
+#pragma unroll
+      for (int j = 0; j < (t < ST - 1 ? T::kCopies + 1 : early); ++j) fetch(t, t * T::kStage, j);
+    wait_vmcnt<(ST - 2) * (T::kCopies + 1) + early>();
+    lds_barrier();
+    read_w(0, 0);
+    read_bs(0);
+#pragma unroll
+    for (int x = 0; x < XB; ++x) read_x(0, x);
+    const int full = q.K / kBlock;
+    int st = 0, before = (ST - 1) * T::kStage;
+    for (int t = 0; t < full; ++t) {
+      const int next = st == (ST - 1) * T::kStage ? 0 : st + T::kStage;
+      step(t, st, next, before);
+      before = st;
+      st = next;
+    }
+    // the last rows of the step before, and a half block (its operands' upper halves zero)
+#pragma unroll
+    for (int i = kSteps - 4; i < kSteps; ++i) fold(i);
+    if (full < blocks) {
+      wait_vmcnt<0>();
+      lds_barrier();
+      const i32x4 none = {0, 0, 0, 0};
+      bs = *reinterpret_cast<const float*>(t0 + st);
+      i32x8 xh[XB];
+#pragma unroll
+      for (int x = 0; x < XB; ++x) {
+        s[x] = *reinterpret_cast<const float*>(s0 + st + 64 * x) * bs;
+        xh[x] = __builtin_shufflevector(
+            *reinterpret_cast<const i32x4*>(a0 + o0 + st + 16 * x * kBlock), none, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+#pragma unroll
+      for (int y = 0; y < YB; ++y) {
+        const i32x8 w = __builtin_shufflevector(
+            *reinterpret_cast<const i32x4*>(b0 + o0 + st + 16 * y * kBlock), none, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int x = 0; x < XB; ++x) {
+          const f32x4 r = block_product(w, xh[x]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[x][y][e] = __builtin_fmaf(r[e], s[x], acc[x][y][e]);
+        }
+      }
+    }
+    wait_vmcnt<0>();  // copies past the last step land before the workgroup ends
+  }
+
+  const bool wide = q.ldc % 4 == 0 && (uintptr_t)q.c % 8 == 0 && n0 + T::BN <= q.N;
+#pragma unroll
+  for (int x = 0; x < XB; ++x) {
+    const int64_t row = m0 + wm + 16 * x + col;
+    if (row >= q.M) continue;
+    uint16_t* to = q.c + row * q.ldc + n0 + wn + 4 * grp;
+    if (wide) {
+#pragma unroll
+      for (int y = 0; y < YB; ++y) {
+        u16x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = bf16_rne(acc[x][y][e]);
+        *reinterpret_cast<u16x4*>(to + 16 * y) = o;
+      }
+    } else {
+#pragma unroll
+      for (int y = 0; y < YB; ++y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n0 + wn + 16 * y + 4 * grp + e < q.N) to[16 * y + e] = bf16_rne(acc[x][y][e]);
+    }
+  }
+}
+
+// The call's first columns in tiles of T, the others in tiles of U: the workgroups
+// before `first_u` take the former.
+using WideT = Wide<4, 2, 4, 8, 2, 2>;  // 256 x 256
+using WideU = Wide<4, 2, 4, 4, 3, 2>;  // 256 x 128
+
+__global__ __launch_bounds__(WideT::kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void linear_fp8_wide_kernel(
+    Call q, int tiles_m, int tiles_t, int tiles_u, uint32_t first_u, int xcd_shift) {
+  int64_t m0;
+  int n0;
+  if (blockIdx.x < first_u) {
+    if (tile_of(blockIdx.x, tiles_m, tiles_t, xcd_shift, WideT::BM, WideT::BN, m0, n0))
+      wide_tile<WideT>(q, m0, n0);
+  } else if (tile_of(blockIdx.x - first_u, tiles_m, tiles_u, xcd_shift, WideU::BM, WideU::BN, m0, n0)) {
+    wide_tile<WideU>(q, m0, tiles_t * WideT::BN + n0);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The kernel for few rows: a workgroup computes 16 XB rows x 16 YB columns over all of
+// K, its kParts wavefronts each one block in kParts.  A block's sum does not depend on the
+// others, only the chain of multiply-adds does: the wavefronts put their blocks' sums
+// and scales into LDS, kDeep blocks each at a time, and one wavefront per 16 x 16 tile
+// runs the chain over them in K's order.  Weights and activations go straight from
+// memory to the matrix core's registers; the next blocks' are asked for before the
+// exchange of the present ones.
+// ---------------------------------------------------------------------------
+template <int XB_, int YB_, int kDeep_, int kParts_>
+struct Narrow {
+  static constexpr int XB = XB_, YB = YB_, kDeep = kDeep_, kParts = kParts_;
+  static constexpr int kThreads = 64 * kParts, kTiles = XB * YB;
+  static constexpr int kRound = kDeep * kParts;            // blocks between two barriers
+  static constexpr int kSums = kRound * kTiles * 1024;     // bytes of a round's sums
+  static constexpr int kBuffer = kSums + kRound * XB * 64;  // and scales
+  static constexpr int BM = 16 * XB, BN = 16 * YB;
+  static_assert(kTiles <= kParts, "a wavefront per tile runs the chain");
+  static_assert(kBlock % BN == 0, "columns of one block of the weights' scales");
+  static_assert(2 * kBuffer <= 160 * 1024, "LDS of a compute unit");
+};
+
+template <class T>
+__global__ __launch_bounds__(T::kThreads) void linear_fp8_narrow_kernel(Call q, int tiles_m) {
+  constexpr int XB = T::XB, YB = T::YB;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int wave = uni(threadIdx.x >> 6);
+  const int lane = __lane_id(), col = lane & 15, grp = lane >> 4;
+  const int64_t m0 = (int64_t)(blockIdx.x % tiles_m) * T::BM;  // rows that share weights are neighbours
+  const int n0 = (int)(blockIdx.x / tiles_m) * T::BN;
+  const int blocks = (q.K + kBlock - 1) / kBlock;
+
+  const uint8_t *a[XB], *b[YB];
+  const float* as[XB];
+#pragma unroll
+  for (int x = 0; x < XB; ++x) {
+    const int64_t r = m0 + 16 * x + col < q.M ? m0 + 16 * x + col : q.M - 1;
+    a[x] = q.a + r * q.lda + 16 * grp;
+    as[x] = q.as + r * q.as_row;
+  }
+#pragma unroll
+  for (int y = 0; y < YB; ++y) {
+    const int r = n0 + 16 * y + col < q.N ? n0 + 16 * y + col : q.N - 1;
+    b[y] = q.b + (int64_t)r * q.ldb + 16 * grp;
+  }
+  const float* bs = q.bs + (int64_t)(n0 / kBlock) * q.bs_row;
+
+  i32x4 alo[T::kDeep][XB], ahi[T::kDeep][XB], blo[T::kDeep][YB], bhi[T::kDeep][YB];
+  float sa[T::kDeep][XB], sb[T::kDeep];
+  const i32x4 none = {0, 0, 0, 0};
+  // block d of this wavefront in the round from block k on (past the last: that one, and
+  // of the half block: its first half again, not used)
+  auto load = [&](int k, int d) {
+    const int blk = min(k + T::kParts * d + wave, blocks - 1);
+    const int64_t at = (int64_t)blk * kBlock;
+    const bool whole = at + kBlock <= q.K;
+    const int64_t up = whole ? at + 64 : at;
+#pragma unroll
+    for (int y = 0; y < YB; ++y) {
+      blo[d][y] = *reinterpret_cast<const i32x4*>(b[y] + at);
+      bhi[d][y] = *reinterpret_cast<const i32x4*>(b[y] + up);
+    }
+#pragma unroll
+    for (int x = 0; x < XB; ++x) {
+      alo[d][x] = *reinterpret_cast<const i32x4*>(a[x] + at);
+      ahi[d][x] = *reinterpret_cast<const i32x4*>(a[x] + up);
+      sa[d][x] = as[x][blk * q.as_blk];
+    }
+    sb[d] = bs[blk * q.bs_blk];
+  };
+
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  if (blocks > 0) {
+#pragma unroll
+    for (int d = 0; d < T::kDeep; ++d) load(0, d);
+  }
+  int buffer = 0;
+  for (int k = 0; k < blocks; k += T::kRound, buffer ^= T::kBuffer) {
+    f32x4* sums = reinterpret_cast<f32x4*>(lds + buffer);
+    float* scales = reinterpret_cast<float*>(lds + buffer + T::kSums);
+#pragma unroll
+    for (int d = 0; d < T::kDeep; ++d) {
+      const int slot = T::kParts * d + wave;
+      const bool half = (k + slot + 1) * kBlock > q.K;  // (or past the last: not used)
+#pragma unroll
+      for (int x = 0; x < XB; ++x) {
+        const i32x8 xa = __builtin_shufflevector(alo[d][x], half ? none : ahi[d][x], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int y = 0; y < YB; ++y) {
+          const i32x8 w = __builtin_shufflevector(blo[d][y], half ? none : bhi[d][y], 0, 1, 2, 3, 4, 5, 6, 7);
+          sums[(slot * T::kTiles + x * YB + y) * 64 + lane] = block_product(w, xa);
+        }
+        if (grp == 0) scales[(slot * XB + x) * 16 + col] = sa[d][x] * sb[d];
+      }
+      if (k + T::kRound < blocks) load(k + T::kRound, d);
+    }
+    lds_barrier();
+    if (wave < T::kTiles) {
+      const int count = min(T::kRound, blocks - k);
+      auto link = [&](int slot) {
+        const f32x4 p = sums[(slot * T::kTiles + wave) * 64 + lane];
+        const float s = scales[(slot * XB + wave / YB) * 16 + col];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(p[e], s, acc[e]);
+      };
+      if (count == T::kRound) {
+#pragma unroll
+        for (int slot = 0; slot < T::kRound; ++slot) link(slot);
+      } else {
+        for (int slot = 0; slot < count; ++slot) link(slot);
+      }
+    }
+  }
+
+  if (wave >= T::kTiles) return;
+  const int64_t row = m0 + 16 * (wave / YB) + col;
+  const int cn = n0 + 16 * (wave % YB) + 4 * grp;
+  if (row >= q.M) return;
+  uint16_t* to = q.c + row * q.ldc + cn;
+  if (q.ldc % 4 == 0 && (uintptr_t)q.c % 8 == 0 && cn + 4 <= q.N) {
+    u16x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = bf16_rne(acc[e]);
+    *reinterpret_cast<u16x4*>(to) = o;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (cn + e < q.N) to[e] = bf16_rne(acc[e]);
+  }
+}
+
 // Workgroups for the output tiles of bm x bn (M, N > 0), a multiple of the dies, or
 // -1 when a grid cannot hold them: the runtime counts a launch's threads in 32
 // bits, and a larger grid wraps.
@@ -267,6 +697,37 @@ int64_t grid_blocks(const Call& x, int bm, int bn, int threads, int xcds) {
   if (tiles_m > UINT32_MAX / tiles_n) return -1;
   const int64_t blocks = (tiles_m * tiles_n + xcds - 1) / xcds * xcds;
   return blocks * threads <= UINT32_MAX ? blocks : -1;
+}
+
+// `tiles_t` column tiles of WideT, and WideU's for the columns behind them.
+int launch_wide(const Call& x, int64_t tiles_t, hipStream_t stream) {
+  const Geometry geo = device_geometry();
+  const int64_t tiles_m = (x.M - 1) / WideT::BM + 1;
+  const int64_t rest = x.N - tiles_t * WideT::BN;
+  const int64_t tiles_u = rest > 0 ? (rest - 1) / WideU::BN + 1 : 0;
+  const int64_t first_u = (tiles_m * tiles_t + geo.xcds - 1) / geo.xcds * geo.xcds;
+  const int64_t blocks = first_u + (tiles_m * tiles_u + geo.xcds - 1) / geo.xcds * geo.xcds;
+  if (blocks * WideT::kThreads > UINT32_MAX) return VD_ERR_INVALID_ARG;
+  constexpr int lds = WideT::kLds > WideU::kLds ? WideT::kLds : WideU::kLds;
+  static std::atomic<unsigned char> lds_set[kMaxDevices];
+  if (set_lds_limit(reinterpret_cast<const void*>(&linear_fp8_wide_kernel), lds, lds_set) != hipSuccess)
+    return VD_ERR_LAUNCH;
+  hipLaunchKernelGGL(linear_fp8_wide_kernel, dim3((unsigned)blocks), dim3(WideT::kThreads), lds, stream,
+                     x, (int)tiles_m, (int)tiles_t, (int)tiles_u, (uint32_t)first_u, geo.xcd_shift);
+  return hipGetLastError() == hipSuccess ? VD_OK : VD_ERR_LAUNCH;
+}
+
+template <class T>
+int launch_narrow(const Call& x, hipStream_t stream) {
+  const int64_t tiles_m = (x.M - 1) / T::BM + 1;
+  const int64_t blocks = grid_blocks(x, T::BM, T::BN, T::kThreads, 1);
+  if (blocks < 0) return VD_ERR_INVALID_ARG;
+  static std::atomic<unsigned char> lds_set[kMaxDevices];
+  if (set_lds_limit(reinterpret_cast<const void*>(&linear_fp8_narrow_kernel<T>), 2 * T::kBuffer, lds_set) != hipSuccess)
+    return VD_ERR_LAUNCH;
+  hipLaunchKernelGGL(linear_fp8_narrow_kernel<T>, dim3((unsigned)blocks), dim3(T::kThreads),
+                     2 * T::kBuffer, stream, x, (int)tiles_m);
+  return hipGetLastError() == hipSuccess ? VD_OK : VD_ERR_LAUNCH;
 }
 
 template <class T>
@@ -283,9 +744,49 @@ int launch(const Call& x, hipStream_t stream) {
   return hipGetLastError() == hipSuccess ? VD_OK : VD_ERR_LAUNCH;
 }
 
+// The tile shapes, smallest first, each with the time of one round of its tiles (a
+// tile per CU of 256 at K = 4096, in us, launches back to back in a graph).  A call
+// takes about ceil(tiles / CUs) rounds; the choice reaches no value.
+#define VD_FP8_SHAPES(X)                                \
+  X(16, 16, launch_narrow<VD_T(Narrow<1, 1, 1, 16>)>, 6.1f)         \
+  X(16, 32, launch<VD_T(Tile<1, 2, 1, 1, 512, 4, 1>)>, 7.7f)        \
+  X(32, 32, launch<VD_T(Tile<1, 2, 2, 1, 512, 3, 1>)>, 9.8f)        \
+  X(64, 64, launch<VD_T(Tile<2, 4, 2, 1, 256, 4, 1>)>, 10.8f)       \
+  X(64, 128, launch<VD_T(Tile<2, 4, 2, 2, 256, 3, 1>)>, 15.4f)      \
+  X(128, 128, launch<VD_T(Tile<4, 2, 2, 4, 128, 4, 1>)>, 23.0f)
+#define VD_T(...) __VA_ARGS__
+constexpr float kRoundT = 55.0f, kRoundU = 34.5f;  // of WideT and WideU
+
 int run(const Call& x, hipStream_t stream) {
-  if (x.M <= 64) return launch<Tile<1, 4, 4, 1, 256, 3, 1>>(x, stream);
-  return launch<Tile<2, 2, 4, 4, 128, 2, 1>>(x, stream);
+  const Geometry geo = device_geometry();
+  const auto rounds = [&](int64_t tiles) { return (float)((tiles + geo.cus - 1) / geo.cus); };
+  float best = 0.0f;
+  int (*fn)(const Call&, hipStream_t) = nullptr;
+  const auto consider = [&](int bm, int bn, int (*f)(const Call&, hipStream_t), float round_us) {
+    const int64_t tiles_m = (x.M - 1) / bm + 1, tiles_n = (x.N - 1) / bn + 1;
+    if (tiles_m > (UINT32_MAX / 1024 - 8) / tiles_n) return;  // (a launch's threads are counted in 32 bits)
+    const float t = rounds(tiles_m * tiles_n) * round_us;
+    if (!fn || t < best) {
+      best = t;
+      fn = f;
+    }
+  };
+#define VD_FP8_CONSIDER(bm, bn, f, us) consider(bm, bn, &f, us);
+  VD_FP8_SHAPES(VD_FP8_CONSIDER)
+#undef VD_FP8_CONSIDER
+  // The wide tiles: all columns in tiles of T, or whole rounds of them and the columns
+  // behind in tiles of U, whichever takes less.
+  const int64_t tiles_m = (x.M - 1) / WideT::BM + 1, all = (x.N - 1) / WideT::BN + 1;
+  if (tiles_m > (UINT32_MAX / WideT::kThreads - 64) / (2 * all)) return fn ? fn(x, stream) : VD_ERR_INVALID_ARG;
+  const auto wide_us = [&](int64_t tiles_t) {
+    const int64_t rest = x.N - tiles_t * WideT::BN;
+    return rounds(tiles_m * tiles_t) * kRoundT + (rest > 0 ? rounds(tiles_m * ((rest - 1) / WideU::BN + 1)) * kRoundU : 0.0f);
+  };
+  int64_t tiles_t = all;
+  for (const int64_t n : {tiles_m * all / geo.cus * geo.cus / tiles_m, (int64_t)0})
+    if (wide_us(n) < wide_us(tiles_t)) tiles_t = n;
+  if (fn && best <= wide_us(tiles_t)) return fn(x, stream);
+  return launch_wide(x, tiles_t, stream);
 }
 
 }  // namespace
@@ -302,6 +803,7 @@ extern "C" int vd_linear_fp8(const void* a, int64_t lda, const float* a_scales, 
   if (K > 0) {
     if (!a || !b || !a_scales || !b_scales) return VD_ERR_INVALID_ARG;
     if (lda < K || ldb < K || lda % 16 != 0 || ldb % 16 != 0) return VD_ERR_INVALID_ARG;
+    if (lda > kMaxStride || ldb > kMaxStride) return VD_ERR_INVALID_ARG;
     if (((uintptr_t)a | (uintptr_t)b) % 16 != 0) return VD_ERR_INVALID_ARG;
     if (((uintptr_t)a_scales | (uintptr_t)b_scales) % 4 != 0) return VD_ERR_INVALID_ARG;
     if (as_row < 0 || as_blk < 0 || bs_row < 0 || bs_blk < 0) return VD_ERR_INVALID_ARG;
