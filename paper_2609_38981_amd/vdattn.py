@@ -445,63 +445,78 @@ E4M3 = torch.float8_e4m3fn
 SCALE_BLOCK = 128  # values per scale
 
 
-def _call(fn, what: str, args, t: torch.Tensor, stream):
-    """One C call on t's device (the library launches on the current one), on ``stream``
-    or that device's current stream."""
-    index = t.device.index
-    if index == torch.cuda.current_device():
-        rc = fn(*args, _stream(stream))
+# The handle of a device's current stream (what torch.cuda.current_stream().cuda_stream gives)
+# and the current device, without the objects around them: 3 us of a call that takes 9.
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
+
+
+def _call(fn, what: str, args, device: int, stream):
+    """One C call on ``device`` (the library launches on the current one), on ``stream`` or
+    that device's current stream."""
+    if device == _current_device():
+        rc = fn(*args, _raw_stream(device) if stream is None else stream.cuda_stream)
     else:
-        with torch.cuda.device(index):
-            rc = fn(*args, _stream(stream))
+        with torch.cuda.device(device):
+            rc = fn(*args, _raw_stream(device) if stream is None else stream.cuda_stream)
     if rc != VD_OK:
         raise VdError(rc, what)
 
 
-def _rows(t, name: str, dtype, device=None, shape=None):
-    """A 2-D device tensor whose rows are contiguous (they may be strided)."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
+def _device_of(t, name: str) -> int:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a device tensor" % name)
+    return t.get_device()
+
+
+def _rows(t, name: str, dtype, device: int, shape=None):
+    """Checks a 2-D tensor on ``device`` whose rows are contiguous (they may be strided); its
+    shape and row stride (a single row has none of its own)."""
+    try:
+        rows, cols = got = t.shape
+        ld, step = t.stride()
+        if t.dtype is dtype and (step == 1 or cols <= 1) and t.get_device() == device and (
+                shape is None or got == shape):
+            return rows, cols, ld if rows > 1 else (cols + 15) // 16 * 16
+    except (AttributeError, ValueError):
+        pass
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
         raise TypeError("%s must be a %s device tensor" % (name, dtype))
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError("%s must be 2-D with contiguous rows" % name)
-    if device is not None and t.device != device:
-        raise ValueError("%s must be on %s" % (name, device))
+    if t.get_device() != device:
+        raise ValueError("%s must be on device %d" % (name, device))
     if shape is not None and t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    raise ValueError("%s must be 2-D with contiguous rows" % name)
 
 
-def _ld(t: torch.Tensor) -> int:
-    """The row stride; a single row has none of its own."""
-    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 15) // 16 * 16
-
-
-def _scales(s, name: str, rows: int, K: int, device):
-    """fp32 scales [rows, ceil(K / 128)] of any strides."""
-    if not isinstance(s, torch.Tensor) or not s.is_cuda or s.dtype != torch.float32:
+def _scales(s, name: str, rows: int, K: int, device: int):
+    """Checks fp32 scales [rows, ceil(K / 128)]; their strides, which may be any (1 where the
+    dimension has one entry)."""
+    if not isinstance(s, torch.Tensor) or s.dtype is not torch.float32:
         raise TypeError("%s must be a float32 device tensor" % name)
-    if s.dim() != 2 or s.shape[0] != rows or s.shape[1] != -(-K // SCALE_BLOCK):
-        raise ValueError("%s must be [%d, %d], got %s" % (name, rows, -(-K // SCALE_BLOCK),
-                                                          tuple(s.shape)))
-    if s.device != device:
-        raise ValueError("%s must be on %s" % (name, device))
+    blocks = -(-K // SCALE_BLOCK)
+    if s.shape != (rows, blocks):
+        raise ValueError("%s must be [%d, %d], got %s" % (name, rows, blocks, tuple(s.shape)))
+    if s.get_device() != device:
+        raise ValueError("%s must be on device %d" % (name, device))
+    a, b = s.stride()
+    return a if rows > 1 else 1, b if blocks > 1 else 1
 
 
-def _new_codes(M: int, K: int, device, out, scales):
+def _new_codes(M: int, K: int, like, device: int, out, scales):
     """The 8-bit output of an M x K result: codes, and scales that lie side by side for
-    each block of K (what linear_fp8 reads fastest)."""
+    each block of K (what linear_fp8 reads fastest); with the C arguments for them."""
     if out is None:
-        out = torch.empty((M, K), dtype=E4M3, device=device)
+        out, ld = torch.empty((M, K), dtype=E4M3, device=like.device), (K + 15) // 16 * 16 if M < 2 else K
     else:
-        _rows(out, "out", E4M3, device, (M, K))
+        ld = _rows(out, "out", E4M3, device, (M, K))[2]
     if scales is None:
-        scales = torch.empty((-(-K // SCALE_BLOCK), M), dtype=torch.float32, device=device).t()
+        strides = 1, max(M, 1)
+        scales = torch.empty_strided((M, -(-K // SCALE_BLOCK)), strides, dtype=torch.float32,
+                                     device=like.device)
     else:
-        _scales(scales, "scales", M, K, device)
-    return out, scales
-
-
-def _scale_strides(s: torch.Tensor):
-    return tuple(s.stride(i) if s.shape[i] > 1 else 1 for i in (0, 1))
+        strides = _scales(scales, "scales", M, K, device)
+    return out, scales, (out.data_ptr(), ld, scales.data_ptr(), *strides, M, K)
 
 
 def linear_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
@@ -509,44 +524,42 @@ def linear_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
     """Batch-invariant linear layer on 8-bit matrices (vd_linear_fp8): a [M, K] e4m3 with
     scales [M, ceil(K / 128)], b [N, K] e4m3 with scales [ceil(N / 128), ceil(K / 128)], out
     [M, N] bf16.  Rows may be strided; the scales may have any strides."""
-    lib = load_library()
-    _rows(a, "a", E4M3)
-    _rows(b, "b", E4M3, a.device)
-    M, K = a.shape
-    N = b.shape[0]
-    if b.shape[1] != K:
-        raise ValueError("a is [M, %d] but b is [N, %d]" % (K, b.shape[1]))
-    _scales(a_scales, "a_scales", M, K, a.device)
-    _scales(b_scales, "b_scales", -(-N // SCALE_BLOCK), K, a.device)
+    lib = _lib or load_library()
+    dev = _device_of(a, "a")
+    M, K, lda = _rows(a, "a", E4M3, dev)
+    N, Kb, ldb = _rows(b, "b", E4M3, dev)
+    if Kb != K:
+        raise ValueError("a is [M, %d] but b is [N, %d]" % (K, Kb))
+    a_strides = _scales(a_scales, "a_scales", M, K, dev)
+    b_strides = _scales(b_scales, "b_scales", -(-N // SCALE_BLOCK), K, dev)
     if out is None:
-        out = torch.empty((M, N), dtype=torch.bfloat16, device=a.device)
+        out, ldc = torch.empty((M, N), dtype=torch.bfloat16, device=a.device), N
     else:
-        _rows(out, "out", torch.bfloat16, a.device, (M, N))
+        ldc = _rows(out, "out", torch.bfloat16, dev, (M, N))[2]
     _call(lib.vd_linear_fp8, "vd_linear_fp8",
-          (a.data_ptr(), _ld(a), a_scales.data_ptr(), a_scales.stride(0), a_scales.stride(1),
-           b.data_ptr(), _ld(b), b_scales.data_ptr(), b_scales.stride(0), b_scales.stride(1),
-           out.data_ptr(), _ld(out) if M > 1 else N, M, N, K), a, stream)
+          (a.data_ptr(), lda, a_scales.data_ptr(), *a_strides, b.data_ptr(), ldb, b_scales.data_ptr(),
+           *b_strides, out.data_ptr(), ldc, M, N, K), dev, stream)
     return out
 
 
 def _norm_inputs(x, weight, residual, residual_out):
-    _rows(x, "x", torch.bfloat16)
-    M, K = x.shape
-    if not isinstance(weight, torch.Tensor) or weight.dtype != torch.bfloat16 or not weight.is_cuda:
+    """(device, M, K, the C arguments up to the sum, residual_out)."""
+    dev = _device_of(x, "x")
+    M, K, ldx = _rows(x, "x", torch.bfloat16, dev)
+    if not isinstance(weight, torch.Tensor) or weight.dtype is not torch.bfloat16:
         raise TypeError("weight must be a bf16 device tensor")
-    if weight.shape != (K,) or not weight.is_contiguous() or weight.device != x.device:
+    if weight.shape != (K,) or (K > 1 and weight.stride(0) != 1) or weight.get_device() != dev:
         raise ValueError("weight must be [%d], contiguous, on %s" % (K, x.device))
     if residual is None:
         if residual_out is not None:
             raise ValueError("residual_out needs a residual")
-        return (None, 0), (None, 0), None
-    _rows(residual, "residual", torch.bfloat16, x.device, x.shape)
+        return dev, M, K, (x.data_ptr(), ldx, None, 0, weight.data_ptr()), (None, 0), None
+    ldr = _rows(residual, "residual", torch.bfloat16, dev, (M, K))[2]
     if residual_out is None:
         residual_out = torch.empty((M, K), dtype=torch.bfloat16, device=x.device)
-    else:
-        _rows(residual_out, "residual_out", torch.bfloat16, x.device, x.shape)
-    return ((residual.data_ptr(), _ld(residual)), (residual_out.data_ptr(), _ld(residual_out)),
-            residual_out)
+    lds = _rows(residual_out, "residual_out", torch.bfloat16, dev, (M, K))[2]
+    return (dev, M, K, (x.data_ptr(), ldx, residual.data_ptr(), ldr, weight.data_ptr()),
+            (residual_out.data_ptr(), lds), residual_out)
 
 
 def rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5,
@@ -555,15 +568,12 @@ def rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5,
     """RMS norm of the rows of x [M, K] (vd_rmsnorm), bf16.  With a residual the rows of
     x + residual are normed, and (out, x + residual) is returned; ``residual_out`` may be x or
     the residual.  Rows may be strided."""
-    lib = load_library()
-    (r, ldr), (s, lds), residual_out = _norm_inputs(x, weight, residual, residual_out)
-    M, K = x.shape
+    lib = _lib or load_library()
+    dev, M, K, inputs, sums, residual_out = _norm_inputs(x, weight, residual, residual_out)
     if out is None:
         out = torch.empty((M, K), dtype=torch.bfloat16, device=x.device)
-    else:
-        _rows(out, "out", torch.bfloat16, x.device, x.shape)
-    _call(lib.vd_rmsnorm, "vd_rmsnorm", (x.data_ptr(), _ld(x), r, ldr, weight.data_ptr(), eps, s, lds,
-                                         out.data_ptr(), _ld(out), M, K), x, stream)
+    ldo = _rows(out, "out", torch.bfloat16, dev, (M, K))[2]
+    _call(lib.vd_rmsnorm, "vd_rmsnorm", (*inputs, eps, *sums, out.data_ptr(), ldo, M, K), dev, stream)
     return out if residual is None else (out, residual_out)
 
 
@@ -573,13 +583,10 @@ def rmsnorm_fp8(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5,
                 scales: Optional[torch.Tensor] = None, stream=None):
     """rmsnorm with its result in 8 bits (vd_rmsnorm_fp8): (codes [M, K] e4m3, scales
     [M, ceil(K / 128)]), with a residual (codes, scales, x + residual)."""
-    lib = load_library()
-    (r, ldr), (s, lds), residual_out = _norm_inputs(x, weight, residual, residual_out)
-    M, K = x.shape
-    out, scales = _new_codes(M, K, x.device, out, scales)
-    _call(lib.vd_rmsnorm_fp8, "vd_rmsnorm_fp8",
-          (x.data_ptr(), _ld(x), r, ldr, weight.data_ptr(), eps, s, lds, out.data_ptr(), _ld(out),
-           scales.data_ptr(), *_scale_strides(scales), M, K), x, stream)
+    lib = _lib or load_library()
+    dev, M, K, inputs, sums, residual_out = _norm_inputs(x, weight, residual, residual_out)
+    out, scales, codes = _new_codes(M, K, x, dev, out, scales)
+    _call(lib.vd_rmsnorm_fp8, "vd_rmsnorm_fp8", (*inputs, eps, *sums, *codes), dev, stream)
     return (out, scales) if residual is None else (out, scales, residual_out)
 
 
@@ -588,15 +595,13 @@ def quantize_fp8(x: torch.Tensor, gate: Optional[torch.Tensor] = None,
                  stream=None):
     """The rows of x [M, K] bf16 in 8 bits (vd_quantize_fp8): (codes [M, K] e4m3, scales
     [M, ceil(K / 128)]).  With a gate [M, K], those of silu(gate) * x.  Rows may be strided."""
-    lib = load_library()
-    _rows(x, "x", torch.bfloat16)
-    M, K = x.shape
-    if gate is not None:
-        _rows(gate, "gate", torch.bfloat16, x.device, x.shape)
-    out, scales = _new_codes(M, K, x.device, out, scales)
-    _call(lib.vd_quantize_fp8, "vd_quantize_fp8",
-          (x.data_ptr(), _ld(x), _ptr(gate), 0 if gate is None else _ld(gate), out.data_ptr(),
-           _ld(out), scales.data_ptr(), *_scale_strides(scales), M, K), x, stream)
+    lib = _lib or load_library()
+    dev = _device_of(x, "x")
+    M, K, ldx = _rows(x, "x", torch.bfloat16, dev)
+    gates = (None, 0) if gate is None else (gate.data_ptr(), _rows(gate, "gate", torch.bfloat16, dev,
+                                                                   (M, K))[2])
+    out, scales, codes = _new_codes(M, K, x, dev, out, scales)
+    _call(lib.vd_quantize_fp8, "vd_quantize_fp8", (x.data_ptr(), ldx, *gates, *codes), dev, stream)
     return out, scales
 
 
@@ -618,37 +623,42 @@ def map_pages(q_lens: torch.Tensor, cached_lens: torch.Tensor, free_pages: torch
     that the new tokens need are taken from ``free_pages`` (int32) and written into
     ``page_table`` (int32 [B, stride], in place).  ``total_q_tokens`` rows of slots, the ones
     behind the last request -1."""
-    lib = load_library()
+    lib = _lib or load_library()
+    dev = _device_of(page_table, "page_table")
+
+    def need(t, name, dtype, numel=0):
+        try:
+            if t.dtype is dtype and t.is_contiguous() and t.get_device() == dev and t.numel() >= numel:
+                return
+        except AttributeError:
+            pass
+        _need(t, name, dtype, numel)
+        raise ValueError("%s must be on %s" % (name, page_table.device))
+
     for t, name in ((q_lens, "q_lens"), (cached_lens, "cached_lens"), (free_pages, "free_pages"),
                     (page_table, "page_table")):
-        _need(t, name, torch.int32)
+        need(t, name, torch.int32)
     B, T = q_lens.numel(), int(total_q_tokens)
     if q_lens.dim() != 1 or cached_lens.shape != q_lens.shape:
         raise ValueError("q_lens and cached_lens must be [num_seqs]")
-    if page_table.dim() != 2 or page_table.shape[0] != B:
+    if page_table.dim() != 2 or page_table.size(0) != B:
         raise ValueError("page_table must be [num_seqs, stride]")
-    dev = page_table.device
     if out is None:
-        i32 = torch.empty(3 * B + 2, dtype=torch.int32, device=dev)
-        out = PageMap(i32[:B + 1], i32[B + 1:2 * B + 1],
-                      torch.empty(max(T, 0), dtype=torch.int64, device=dev),
-                      i32[2 * B + 1:3 * B + 1], i32[3 * B + 1:])
+        cu, ctx, status, used = torch.empty(3 * B + 2, dtype=torch.int32, device=page_table.device).split(
+            (B + 1, B, B, 1))
+        out = PageMap(cu, ctx, torch.empty(max(T, 0), dtype=torch.int64, device=page_table.device),
+                      status, used)
     else:
         for t, name, dtype, n in ((out.cu_q_lens, "cu_q_lens", torch.int32, B + 1),
                                   (out.context_lens, "context_lens", torch.int32, B),
                                   (out.slot_mapping, "slot_mapping", torch.int64, T),
                                   (out.status, "status", torch.int32, B),
                                   (out.pages_used, "pages_used", torch.int32, 1)):
-            _need(t, name, dtype, n)
-            if t.device != dev:
-                raise ValueError("%s must be on %s" % (name, dev))
-    for t, name in ((q_lens, "q_lens"), (cached_lens, "cached_lens"), (free_pages, "free_pages")):
-        if t.device != dev:
-            raise ValueError("%s must be on %s" % (name, dev))
+            need(t, name, dtype, n)
     m = _PageMap(B, T, q_lens.data_ptr(), cached_lens.data_ptr(), free_pages.data_ptr(),
                  free_pages.numel(), int(num_pages), page_table.data_ptr(),
-                 page_table.shape[1] if B else 1, out.cu_q_lens.data_ptr(),
+                 page_table.size(1) if B else 1, out.cu_q_lens.data_ptr(),
                  out.context_lens.data_ptr(), out.slot_mapping.data_ptr(), out.status.data_ptr(),
                  out.pages_used.data_ptr())
-    _call(lib.vd_map_pages, "vd_map_pages", (ctypes.byref(m),), page_table, stream)
+    _call(lib.vd_map_pages, "vd_map_pages", (ctypes.byref(m),), dev, stream)
     return out
