@@ -38,6 +38,7 @@ namespace {
 
 constexpr int kGroup = 128;       // values per scale
 constexpr int kMaxNormK = 32768;  // 1024 threads of 4 vectors of 8
+constexpr int64_t kMaxGroups = INT64_C(1) << 27;  // of a launch: its threads are counted in 32 bits
 constexpr float kMinTop = 0x1p-117f;
 constexpr float kPer448 = 1.0f / 448.0f;
 
@@ -167,38 +168,61 @@ struct RowArgs {
   const uint16_t *x, *gate;
   uint8_t* out;
   float* scales;
-  int64_t ldx, ldg, ldo, s_row, s_blk, groups;
-  int K, per_row;  // values and groups of a row
+  int64_t ldx, ldg, ldo, s_row, s_blk;
+  uint32_t groups, per_row;  // groups of all rows and of one
+  int K;
 };
 
-// 16 lanes per group of 128 values, groups in row order.
-template <bool GATE>
+// silu(g) = g / (1 + exp(-g)), by t = exp(-|g|) in [0, 1], so that nothing overflows: g / (1 + t)
+// or g t / (1 + t).  g has 8 bits, so its product with the 16 upper bits of log2(e) / 2 is
+// exact and the rest a correction; t is the square of exp2 of half the exponent, whose
+// results stay normal where t does not.  Within 12 2^-24: exp2 and the reciprocal of the
+// transcendental unit are off by one unit in the last place at most.
+__device__ __forceinline__ float silu(float g) {
+  constexpr float kHalfLog2e = 0.721347520444481703f;
+  constexpr float kUpper = 0x1.715p-1f;  // 13 bits of it
+  const float n = -__builtin_fabsf(g);
+  float h = ex2(n * kUpper);
+  h = __builtin_fmaf(h, n * ((kHalfLog2e - kUpper) * 0.693147180559945309f), h);
+  const float t = h * h;
+  const float r = __builtin_amdgcn_rcpf(1.0f + t);
+  return (g < 0.0f ? g * t : g) * r;
+}
+
+// 16 lanes per group of 128 values, groups in row order; a workgroup takes U times 16 of
+// them, all loads before the arithmetic.
+template <bool GATE, int U>
 __global__ __launch_bounds__(256) void quantize_kernel(RowArgs a) {
   const int lane16 = threadIdx.x & 15;
-  for (int64_t u0 = (int64_t)blockIdx.x * 16; u0 < a.groups; u0 += (int64_t)gridDim.x * 16) {
-    const int64_t u = u0 + (threadIdx.x >> 4);
-    const int64_t row = u / a.per_row;
-    const int g = (int)(u - row * a.per_row);
-    const int k = g * kGroup + 8 * lane16;
-    const bool in = u < a.groups && k < a.K;
-    u16x8 xv = {}, gv = {};
-    if (in) {
-      xv = *reinterpret_cast<const u16x8*>(a.x + row * a.ldx + k);
-      if (GATE) gv = *reinterpret_cast<const u16x8*>(a.gate + row * a.ldg + k);
+  const uint32_t u0 = blockIdx.x * (16u * U) + (threadIdx.x >> 4);
+  u16x8 xv[U], gv[U];
+  uint32_t row[U], g[U];
+  bool in[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const uint32_t u = u0 + 16u * j;
+    row[j] = u / a.per_row;
+    g[j] = u - row[j] * a.per_row;
+    const int k = (int)g[j] * kGroup + 8 * lane16;
+    in[j] = u < a.groups && k < a.K;
+    xv[j] = gv[j] = u16x8{};
+    if (in[j]) {
+      xv[j] = *reinterpret_cast<const u16x8*>(a.x + row[j] * a.ldx + k);
+      if (GATE) gv[j] = *reinterpret_cast<const u16x8*>(a.gate + row[j] * a.ldg + k);
     }
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
     float y[8], scale;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      y[e] = bf16_f32(xv[e]);
-      if (GATE) {
-        const float s = bf16_f32(gv[e]);
-        y[e] = s / (1.0f + expf(-s)) * y[e];
-      }
+      y[e] = bf16_f32(xv[j][e]);
+      if (GATE) y[e] *= silu(bf16_f32(gv[j][e]));
     }
     const u32x2 q = to_codes(y, scale);
-    if (in) {
-      *reinterpret_cast<u32x2*>(a.out + row * a.ldo + k) = q;
-      if (lane16 == 0) a.scales[row * a.s_row + g * a.s_blk] = scale;
+    if (in[j]) {
+      *reinterpret_cast<u32x2*>(a.out + row[j] * a.ldo + (int)g[j] * kGroup + 8 * lane16) = q;
+      if (lane16 == 0) a.scales[row[j] * a.s_row + g[j] * a.s_blk] = scale;
     }
   }
 }
@@ -288,16 +312,24 @@ int vd_quantize_fp8(const void* x, int64_t ldx, const void* gate, int64_t ldg, v
   if (M == 0 || K == 0) return VD_OK;
   const int per_row = (K - 1) / kGroup + 1;
   if (bad_rows(x, ldx, K) || (gate && bad_rows(gate, ldg, K)) ||
-      bad_codes(out, ldo, scales, s_row, s_blk, M, K) || M > INT64_MAX / 2 / per_row)
+      bad_codes(out, ldo, scales, s_row, s_blk, M, K) || M > kMaxGroups / per_row)
     return VD_ERR_INVALID_ARG;
   const RowArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(gate),
-                  static_cast<uint8_t*>(out), scales, ldx, ldg, ldo, s_row, s_blk, M * per_row, K,
-                  per_row};
-  const dim3 grid((unsigned)std::min<int64_t>((a.groups + 15) / 16, 1 << 20));
-  if (gate)
-    hipLaunchKernelGGL(quantize_kernel<true>, grid, dim3(256), 0, stream, a);
+                  static_cast<uint8_t*>(out), scales, ldx, ldg, ldo, s_row, s_blk,
+                  (uint32_t)(M * per_row), (uint32_t)per_row, K};
+  // 4 groups a lane where that leaves several workgroups per CU, else one
+  const bool many = a.groups >= 16u * 4 * 4 * device_geometry().cus;
+  const dim3 grid((a.groups - 1) / (many ? 64 : 16) + 1);
+#define VD_ROWS(GATE, U) hipLaunchKernelGGL((quantize_kernel<GATE, U>), grid, dim3(256), 0, stream, a)
+  if (gate && many)
+    VD_ROWS(true, 4);
+  else if (gate)
+    VD_ROWS(true, 1);
+  else if (many)
+    VD_ROWS(false, 4);
   else
-    hipLaunchKernelGGL(quantize_kernel<false>, grid, dim3(256), 0, stream, a);
+    VD_ROWS(false, 1);
+#undef VD_ROWS
   return hipGetLastError() == hipSuccess ? VD_OK : VD_ERR_LAUNCH;
 }
 
