@@ -374,8 +374,9 @@ int vd_linear(const void* a, int64_t lda, const void* b, int64_t ldb, void* c, i
  * normed after it, and rows do not depend on M.
  * x, residual, sum, out: device rows of K bf16 values (out of vd_rmsnorm_fp8: K codes);
  * weight: K bf16 values.  Strides in elements.  residual and sum go together (both NULL:
- * no addition).  sum may be x or residual and the bf16 out may be x, residual or sum's
- * input (the same pointer and stride: rows in place); other overlaps are not allowed.
+ * no addition).  Rows may be normed in place: sum may be x or residual, and the bf16 out may
+ * be x or residual (the same pointer and stride), but out and sum are two matrices; other
+ * overlaps are not allowed, and the codes overlap no input.
  * Requirements: K a multiple of 8 and at most 32768 (else VD_ERR_UNSUPPORTED); eps finite,
  * >= 0; bf16 rows 16-byte aligned with strides >= K that are multiples of 8; codes 8-byte
  * aligned with a stride >= K that is a multiple of 8; s_row, s_blk >= 1 where M > 1 and
@@ -393,7 +394,8 @@ int vd_rmsnorm_fp8(const void* x, int64_t ldx, const void* residual, int64_t ldr
  *   y[m][k] = gate[m][k] / (1 + exp(-gate[m][k])) * x[m][k]      in fp32
  * (the inner activation of a gated MLP; gate and x may be two column ranges of one matrix).
  * Requirements as for vd_rmsnorm_fp8, with any K that is a multiple of 8; out overlaps
- * neither input.  A row's bits depend on that row only. */
+ * neither input; M * ceil(K / 128) at most 2^27 (VD_ERR_INVALID_ARG).  A row's bits depend on
+ * that row only. */
 int vd_quantize_fp8(const void* x, int64_t ldx, const void* gate, int64_t ldg, void* out,
                     int64_t ldo, float* scales, int64_t s_row, int64_t s_blk, int64_t M, int32_t K,
                     hipStream_t stream);
@@ -412,8 +414,8 @@ int vd_quantize_fp8(const void* x, int64_t ldx, const void* gate, int64_t ldg, v
  * as * bs and added with one rounding (fma), cast to bf16 round-to-nearest-even at the end:
  * row m of c is bit-identical for any M, any position of the row in a, and any strides.
  * Requirements (else VD_ERR_UNSUPPORTED for K, VD_ERR_INVALID_ARG otherwise): K a multiple
- * of 64; when K > 0, lda, ldb >= K and multiples of 16 with a and b 16-byte aligned and
- * scales 4-byte aligned (K = 0: none of them is read and every output is +0); ldc >= N; c
+ * of 64; when K > 0, lda, ldb >= K, at most 2^29 and multiples of 16 with a and b 16-byte
+ * aligned and scales 4-byte aligned (K = 0: none of them is read and every output is +0); ldc >= N; c
  * 2-byte aligned; M, N, K >= 0 (M = 0 or N = 0: nothing to do; VD_ERR_INVALID_ARG past what
  * one launch covers).  c overlaps no input.  Launches on `stream` and returns without waiting;
  * allocates nothing.  Strides are in elements. */

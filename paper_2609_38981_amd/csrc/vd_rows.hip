@@ -248,6 +248,7 @@ int check_norm(const NormArgs& a, int64_t K) {
   if (bad_rows(a.x, a.ldx, a.K) || !a.w || misaligned(a.w, 16)) return VD_ERR_INVALID_ARG;
   if (!a.res != !a.sum) return VD_ERR_INVALID_ARG;
   if (a.res && (bad_rows(a.res, a.ldr, a.K) || bad_rows(a.sum, a.lds, a.K))) return VD_ERR_INVALID_ARG;
+  if (a.out && a.out == a.sum) return VD_ERR_INVALID_ARG;  // (one would overwrite the other)
   return VD_OK;
 }
 

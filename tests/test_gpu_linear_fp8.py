@@ -71,6 +71,32 @@ def test_rows_and_columns_do_not_depend_on_the_call(n, k):
                             full[:m, lo:hi], (m, lo, hi))
 
 
+@pytest.mark.parametrize("m,n,ks", [
+    (10, 4000, (64, 192, 2112)),      # 16 x 16, the blocks of K shared out
+    (10, 6100, (64, 192, 2112)),      # 16 x 32
+    (30, 6100, (64, 192, 1088)),      # 32 x 32
+    (100, 6100, (64, 192, 576)),      # 64 x 64
+    (250, 6000, (64, 192, 576)),      # 64 x 128
+    (500, 6100, (64, 128, 192, 576)),  # 128 x 128
+    (700, 6100, (64, 128, 192, 320, 576)),   # 256 x 128
+    (4095, 4090, (64, 128, 192, 320)),  # 256 x 256
+    (4100, 5000, (64, 128, 192, 320, 1344)),  # 256 x 256, and 256 x 128 for the last columns
+])
+def test_tile_shapes(m, n, ks):
+    """A call of each tile shape on 256 CUs, ragged in M and N, with K of a half block, one, one
+    and a half, and more: sampled rows within the bound; rows alone and the last columns alone
+    (other shapes) bit-identical."""
+    for k in ks:
+        x = a, a_s, b, b_s = _draw(m + k, m, n, k, by_row=k % 128 > 0)
+        full = V.linear_fp8(*x)
+        O.check_linear(full, x, rows=[0, m // 2, m - 1])
+        for lo, hi in [(0, 1), (m // 2, m // 2 + 20), (max(m - 70, 0), m)]:
+            hi = min(hi, m)
+            O.same_bits(V.linear_fp8(a[lo:hi], a_s[lo:hi], b, b_s), full[lo:hi], (k, lo))
+        c = (n - 1) // 128 * 128
+        O.same_bits(V.linear_fp8(a, a_s, b[c:], b_s[c // 128:]), full[:, c:], k)
+
+
 @pytest.mark.parametrize("m", [1, 20, 70, 300])
 def test_strides(m):
     n, k = 333, 448

@@ -171,6 +171,7 @@ def test_wrappers_refuse():
                  (lambda: V.rmsnorm(x, w[:64]), ValueError),
                  (lambda: V.rmsnorm(x, w, residual=x[:2]), ValueError),
                  (lambda: V.rmsnorm(x, w, residual_out=x), ValueError),
+                 (lambda: V.rmsnorm(x, w, residual=x, residual_out=x, out=x), V.VdError),
                  (lambda: V.rmsnorm(x.t(), w), ValueError),
                  (lambda: V.rmsnorm(x, w, eps=-1.0), V.VdError),
                  (lambda: V.rmsnorm(x[:, 4:68], w[:64]), V.VdError),

@@ -35,7 +35,7 @@ def test_every_operator_is_declared(lib):
 
 
 NORM = "x ldx res ldr w eps sum lds out ldo M K".split()
-NORM_OK = dict(x=FAKE, ldx=128, res=FAKE, ldr=128, w=FAKE, eps=1e-5, sum=FAKE, lds=128, out=FAKE,
+NORM_OK = dict(x=FAKE, ldx=128, res=FAKE, ldr=128, w=FAKE, eps=1e-5, sum=FAKE, lds=128, out=FAKE + 4096,
                ldo=128, M=4, K=128)
 NORM8 = "x ldx res ldr w eps sum lds out ldo s s_row s_blk M K".split()
 NORM8_OK = dict(NORM_OK, s=FAKE, s_row=1, s_blk=4)
@@ -50,7 +50,7 @@ def test_norm_rejects_before_launch(lib, fp8):
            dict(x=None), dict(x=FAKE + 8), dict(ldx=120), dict(ldx=132), dict(w=None),
            dict(w=FAKE + 2), dict(res=None), dict(sum=None), dict(ldr=64), dict(lds=64),
            dict(res=FAKE + 4), dict(sum=FAKE + 8), dict(out=None), dict(ldo=64), dict(ldo=130),
-           dict(out=FAKE + 4)]
+           dict(out=FAKE + 4), dict(out=FAKE)]
     if fp8:
         bad += [dict(s=None), dict(s=FAKE + 2), dict(s_row=0), dict(s_row=-1),
                 dict(K=256, ldx=256, ldr=256, lds=256, ldo=256, s_blk=0)]
@@ -72,7 +72,7 @@ def test_quantize_rejects_before_launch(lib):
     for kw in (dict(M=-1), dict(K=-8), dict(x=None), dict(x=FAKE + 2), dict(ldx=248), dict(ldx=260),
                dict(gate=FAKE + 8), dict(ldg=8), dict(ldg=257), dict(out=None), dict(out=FAKE + 4),
                dict(ldo=255), dict(ldo=260), dict(s=None), dict(s=FAKE + 1), dict(s_row=0),
-               dict(s_blk=0), dict(s_blk=-4), dict(M=2**62)):
+               dict(s_blk=0), dict(s_blk=-4), dict(M=2**62), dict(M=2**26 + 1)):
         assert call(**kw) == -1, kw
     assert call(K=252) == -2
 
@@ -86,7 +86,7 @@ def test_linear_fp8_rejects_before_launch(lib):
     assert call(M=0) == 0 and call(N=0) == 0
     bad = [dict(M=-1), dict(N=-1), dict(K=-1), dict(c=None), dict(ldc=8), dict(c=FAKE + 1),
            dict(a=None), dict(b=None), dict(bs=None), {"as": None}, dict(lda=64), dict(ldb=64),
-           dict(lda=136), dict(ldb=132), dict(a=FAKE + 8), dict(b=FAKE + 4), {"as": FAKE + 2},
+           dict(lda=136), dict(ldb=132), dict(lda=2**29 + 16), dict(ldb=2**30), dict(a=FAKE + 8), dict(b=FAKE + 4), {"as": FAKE + 2},
            dict(bs=FAKE + 1), dict(as_row=-1), dict(as_blk=-1), dict(bs_row=-1), dict(bs_blk=-1)]
     for kw in bad:
         assert call(**kw) == -1, kw
