@@ -16,18 +16,27 @@
 // exponent sum of the 8: at most 7 2^-13 of the largest of them are lost, about
 // 2^-14 of a result of random codes against the 2^-8 that its bf16 rounding may
 // take.  The steps that keep every bit of the products (the codes widened to bf16)
-// run at half its rate, less the widening.  The last block of K = 64 (mod 128) is filled with zeros.  A
-// cell of the matrix step depends only on its own row of either operand, so the
-// tile, the workgroup and the other rows of the call reach no bits.
+// run at half its rate, less the widening.  The last block of K = 64 (mod 128) is
+// filled with zeros.  A cell of the matrix step depends only on its own row of either
+// operand, so the tile, the workgroup and the other rows of the call reach no bits.
 //
 // Weights are the first operand (rows of the step), so a lane's four results are
 // neighbours of one output row and share the activation's scale.  Operand of lane
 // (col = l & 15, grp = l >> 4): bytes 16 grp .. + 15 and 64 + 16 grp .. + 15 of row
 // col's block, for both operands alike.
+//
+// Three kernels, chosen by M, N and K (run): for one round of the smallest tiles the
+// wavefronts of a workgroup share K's blocks; tiles of 16 x 32 to 128 x 128 with a ring
+// of LDS stages, for calls that are bound by the weights' bytes and a workgroup's chain of
+// steps; tiles of 256 x 128 and 256 x 256 for calls bound by the matrix cores.
+// Measured (us a call back to back in a graph; floors: the bytes at 6.4 TB/s, or the
+// operations at 2.8 PFLOP/s, a large library product's rate on unscaled codes): 1 x 4096
+// x 4096 6.1 (floor 2.6), 48 x 6144 x 4096 10.1 (4.1), 333 x 5000 x 2112 11.6 (2.5), 4096 x
+// 6144 x 4096 109 (74), 4096 x 28672 x 8192 805 (687: 2.39 PFLOP/s).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
-#include <type_traits>
+#include <initializer_list>
 
 #include "../../include/vdattn.h"
 #include "vd_cas.hpp"
@@ -44,7 +53,6 @@ constexpr int64_t kMaxStride = INT64_C(1) << 29;  // 7 rows within 32 bits of a 
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // One block of one 16 x 16 tile: rows of the weights, columns of the activations.
 __device__ __forceinline__ f32x4 block_product(const i32x8& w, const i32x8& x) {
@@ -64,9 +72,9 @@ struct Call {
 
 // One tile shape: WM x WN wavefronts, each computing XB x YB steps of 16 x 16 (XB
 // over activations); K advances BK bytes per step through an LDS ring of ST stages.
-template <int WM_, int WN_, int XB_, int YB_, int BK_, int ST_, int EU_>
+template <int WM_, int WN_, int XB_, int YB_, int BK_, int ST_>
 struct Tile {
-  static constexpr int WM = WM_, WN = WN_, XB = XB_, YB = YB_, BK = BK_, ST = ST_, EU = EU_;
+  static constexpr int WM = WM_, WN = WN_, XB = XB_, YB = YB_, BK = BK_, ST = ST_;
   static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
   static constexpr int BM = WM * 16 * XB;   // rows of a per workgroup tile
   static constexpr int BN = WN * 16 * YB;   // rows of b per tile
@@ -108,7 +116,7 @@ __device__ __forceinline__ bool tile_of(uint32_t block, int tiles_m, int tiles_n
 }
 
 template <class T>
-__global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(T::EU, T::EU))) void linear_fp8_kernel(
+__global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(1, 2))) void linear_fp8_kernel(
     Call q, int tiles_m, int tiles_n, int xcd_shift) {
   constexpr int XB = T::XB, YB = T::YB, ST = T::ST;
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -155,23 +163,21 @@ __global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(T::
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int steps = (blocks + T::kBlocks - 1) / T::kBlocks;
-  // copy j of block c of a step (the last one: scales); blocks and chunks past K
-  // repeat the last ones, in bounds and never used
-  auto fetch_one = [&](int step, int c, int j) {
-    const int blk = min(step * T::kBlocks + c, blocks - 1);
-    const uint32_t at = lds0 + (step % ST) * T::kStage + c * T::kStageBlock;
-    const uint32_t back = blk * kBlock + kBlock > q.K ? ck & 64 : 0;
-    if (j < T::kTileCopies)
-      lds_dma16_at(src[j] + (int64_t)blk * kBlock, off[j] - back,
-                   uni((int)(at + 1024 * (wave * T::kTileCopies + j))));
-    else
-      lds_dma4(scale_src + blk * scale_step, uni((int)(at + T::kTileA + T::kTileB + 256 * wave)));
-  };
+  // this wavefront's copies of a step; blocks and chunks past K repeat the last ones, in
+  // bounds and never used
   auto fetch = [&](int step) {
+    const uint32_t st = lds0 + (step % ST) * T::kStage;
 #pragma unroll
-    for (int c = 0; c < T::kBlocks; ++c)
+    for (int c = 0; c < T::kBlocks; ++c) {
+      const int blk = min(step * T::kBlocks + c, blocks - 1);
+      const uint32_t at = st + c * T::kStageBlock;
+      const uint32_t back = blk * kBlock + kBlock > q.K ? ck & 64 : 0;
 #pragma unroll
-      for (int j = 0; j <= T::kTileCopies; ++j) fetch_one(step, c, j);
+      for (int j = 0; j < T::kTileCopies; ++j)
+        lds_dma16_at(src[j] + (int64_t)blk * kBlock, off[j] - back,
+                     uni((int)(at + 1024 * (wave * T::kTileCopies + j))));
+      lds_dma4(scale_src + blk * scale_step, uni((int)(at + T::kTileA + T::kTileB + 256 * wave)));
+    }
   };
 
   // this wavefront's part: rows wm .. + 16 XB - 1 of a, wn .. + 16 YB - 1 of b
@@ -184,58 +190,45 @@ __global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(T::
 #pragma unroll
     for (int y = 0; y < YB; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // One block of K.  The fused multiply-adds of a row of tiles are issued between the
-  // matrix steps of the next one, whose weights are read a row ahead: a matrix step
-  // holds the core for 32 cycles, four multiply-adds the vector unit for 16.  The
-  // last row's wait for the next block, behind its operand reads and the copies.
-  f32x4 p[2][XB];
-  float s[XB];
-  auto fold = [&](int y) {
+  // One step: the operands of all its blocks are read before its first product, so that
+  // one latency of LDS and of the matrix core covers the step; the chains come last.
+  // half: the last of `count` blocks ends after 64 values, the rest of it counts as zeros.
+  const int o0 = (grp ^ (col & 7)) << 4, o1 = ((4 + grp) ^ (col & 7)) << 4;
+  auto compute = [&](const char* stage, int count, bool half, auto copies) {
+    i32x8 xa[T::kBlocks][XB], wv[T::kBlocks][YB];
+    float s[T::kBlocks][XB];
 #pragma unroll
-    for (int x = 0; x < XB; ++x)
+    for (int c = 0; c < T::kBlocks; ++c) {
+      const char* st = stage + c * T::kStageBlock;
+      const float* S = reinterpret_cast<const float*>(st + T::kTileA + T::kTileB);
+      const bool cut = half && c == count - 1;
+      auto operand = [&](const char* row) {
+        const i32x4 lo = *reinterpret_cast<const i32x4*>(row + o0);
+        i32x4 hi = *reinterpret_cast<const i32x4*>(row + o1);
+        if (cut) hi = i32x4{0, 0, 0, 0};
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      };
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[x][y][e] = __builtin_fmaf(p[y & 1][x][e], s[x], acc[x][y][e]);
-  };
-  auto block = [&](const char* st, bool half, auto copies) {
-    const char* TA = st;
-    const char* TB = st + T::kTileA;
-    const float* S = reinterpret_cast<const float*>(st + T::kTileA + T::kTileB);
-    const int o0 = (grp ^ (col & 7)) << 4, o1 = ((4 + grp) ^ (col & 7)) << 4;
-    auto operand = [&](const char* row) {
-      const i32x4 lo = *reinterpret_cast<const i32x4*>(row + o0);
-      i32x4 hi = *reinterpret_cast<const i32x4*>(row + o1);
-      if (half) hi = i32x4{0, 0, 0, 0};
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    i32x8 xa[XB], wv[2];
-    wv[0] = operand(TB + (wn + col) * kBlock);
+      for (int y = 0; y < YB; ++y) wv[c][y] = operand(st + T::kTileA + (wn + 16 * y + col) * kBlock);
 #pragma unroll
-    for (int x = 0; x < XB; ++x) xa[x] = operand(TA + (wm + 16 * x + col) * kBlock);
-    const float bs = S[64 * T::kScaleWaves + nb];
-    float ns[XB];
+      for (int x = 0; x < XB; ++x) xa[c][x] = operand(st + (wm + 16 * x + col) * kBlock);
+      const float bs = S[64 * T::kScaleWaves + nb];
 #pragma unroll
-    for (int x = 0; x < XB; ++x) ns[x] = S[wm + 16 * x + col];
-    __builtin_amdgcn_sched_barrier(0);
-    copies();
-    fold(YB - 1);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int x = 0; x < XB; ++x) s[x] = ns[x] * bs;
-#pragma unroll
-    for (int y = 0; y < YB; ++y) {
-      if (y + 1 < YB) wv[(y + 1) & 1] = operand(TB + (wn + 16 * (y + 1) + col) * kBlock);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int x = 0; x < XB; ++x) {
-        p[y & 1][x] = block_product(wv[y & 1], xa[x]);
-        if (y > 0) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc[x][y - 1][e] = __builtin_fmaf(p[(y - 1) & 1][x][e], s[x], acc[x][y - 1][e]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      for (int x = 0; x < XB; ++x) s[c][x] = S[wm + 16 * x + col] * bs;
     }
+    copies();
+#pragma unroll
+    for (int c = 0; c < T::kBlocks; ++c)
+      if (c < count) {
+#pragma unroll
+        for (int y = 0; y < YB; ++y)
+#pragma unroll
+          for (int x = 0; x < XB; ++x) {
+            const f32x4 p = block_product(wv[c][y], xa[c][x]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[x][y][e] = __builtin_fmaf(p[e], s[c][x], acc[x][y][e]);
+          }
+      }
   };
 
   // One barrier per step: after it, step t's copies are visible to every
@@ -253,27 +246,10 @@ __global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(T::
     lds_barrier();
     return (const char*)lds + (t % ST) * T::kStage;
   };
-#pragma unroll
-  for (int x = 0; x < XB; ++x) {
-    s[x] = 0.0f;
-    p[(YB - 1) & 1][x] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  for (int t = 0; t < full; ++t) {
-    const char* st = begin(t);
-#pragma unroll
-    for (int c = 0; c < T::kBlocks; ++c)
-      block(st + c * T::kStageBlock, false, [&] {
-#pragma unroll
-        for (int j = 0; j <= T::kTileCopies; ++j) fetch_one(t + ST - 1, c, j);
-      });
-  }
-  if (full < steps) {
-    const char* st = begin(full);
-    for (int c = 0; full * T::kBlocks + c < blocks; ++c)
-      block(st + c * T::kStageBlock, (full * T::kBlocks + c + 1) * kBlock > q.K, [] {});
-  }
+  for (int t = 0; t < full; ++t)
+    compute(begin(t), T::kBlocks, false, [&] { fetch(t + ST - 1); });
+  if (full < steps) compute(begin(full), blocks - full * T::kBlocks, q.K % kBlock != 0, [] {});
   wait_vmcnt<0>();
-  fold(YB - 1);
 
   // result e of tile (x, y) in lane (col, grp): row 16 x + col, column 16 y + 4 grp + e
   const bool wide = q.ldc % 4 == 0 && (uintptr_t)q.c % 8 == 0;
@@ -301,15 +277,22 @@ __global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(T::
 
 // ---------------------------------------------------------------------------
 // The kernel for many rows: tiles of WM x WN wavefronts of XB x YB steps each, a
-// block of K per step, two stages of LDS (A0 A1 B0 B1 S0 S1).
+// block of K per step, ST stages of LDS.
 //
-// A step's operand reads, matrix steps, multiply-adds and copies all run beside
-// each other: the activations of step t + 1 are read into registers of their own
-// during the last row of step t, the weights a row ahead, and a row's
-// multiply-adds are issued between the matrix steps of the next row.  The one
-// barrier stands before the last row: there every wavefront has read all of stage
-// t (the copies of t + 2 refill it) and its copies of t + 1, issued a step ago,
-// have landed.
+// Operand reads, matrix steps, multiply-adds and copies run beside each other: a matrix
+// step holds the core for 32 cycles, the four multiply-adds of an earlier one the
+// vector unit for 16; the weights are read 2 to 3 rows of tiles ahead, the next
+// step's activations during the last kLast rows.  The one barrier of a step stands before
+// those: there every wavefront has read all of stage t (the copies of t + ST refill it,
+// one every kPer matrix steps) and its copies of t + 1 have landed.
+//
+// What bounds it, 4096 x 28672 x 8192 in 256 x 256 tiles: without the multiply-adds it
+// takes 743 us, without the copies 657, without both 568, all of it 800; the matrix cores
+// are busy 58% of the cycles at the 1.98 GHz that the power allows (the library's
+// unscaled product: 85% at 1.76 GHz, 610 us).  The same steps without the reads ahead 865; as
+// 32 x 32 x 64 steps 905; kLast 1, 2, 3 with the best kPer of each 803, 800, 800; copies of a
+// in a phase of their own behind a second barrier 850; 128 x 128 tiles, two workgroups
+// a CU 1075.
 // ---------------------------------------------------------------------------
 template <int WM_, int WN_, int XB_, int YB_, int ST_, int kPer_>
 struct Wide {
@@ -542,7 +525,8 @@ __device__ __forceinline__ void wide_tile(const Call& q, int64_t m0, int n0) {
 }
 
 // The call's first columns in tiles of T, the others in tiles of U: the workgroups
-// before `first_u` take the former.
+// before `first_u` take the former.  Whole rounds of T and the rest in U: 4096 x 6144 x
+// 4096 109 us in a graph, T alone 124, U alone 121.
 using WideT = Wide<4, 2, 4, 8, 2, 2>;  // 256 x 256
 using WideU = Wide<4, 2, 4, 4, 3, 2>;  // 256 x 128
 
@@ -561,19 +545,17 @@ __global__ __launch_bounds__(WideT::kThreads) __attribute__((amdgpu_waves_per_eu
 // ---------------------------------------------------------------------------
 // The kernel for few rows: a workgroup computes 16 XB rows x 16 YB columns over all of
 // K, its kParts wavefronts each one block in kParts.  A block's sum does not depend on the
-// others, only the chain of multiply-adds does: the wavefronts put their blocks' sums
-// and scales into LDS, kDeep blocks each at a time, and one wavefront per 16 x 16 tile
-// runs the chain over them in K's order.  Weights and activations go straight from
-// memory to the matrix core's registers; the next blocks' are asked for before the
-// exchange of the present ones.
+// others, only the chain of multiply-adds does: a round at a time the wavefronts put their
+// blocks' sums and scales into LDS, and one wavefront per 16 x 16 tile runs the chain
+// over them in K's order.  Weights and activations go straight from memory to the
+// matrix core's registers, kDeep rounds ahead.
 // ---------------------------------------------------------------------------
 template <int XB_, int YB_, int kDeep_, int kParts_>
 struct Narrow {
   static constexpr int XB = XB_, YB = YB_, kDeep = kDeep_, kParts = kParts_;
   static constexpr int kThreads = 64 * kParts, kTiles = XB * YB;
-  static constexpr int kRound = kDeep * kParts;            // blocks between two barriers
-  static constexpr int kSums = kRound * kTiles * 1024;     // bytes of a round's sums
-  static constexpr int kBuffer = kSums + kRound * XB * 64;  // and scales
+  static constexpr int kSums = kParts * kTiles * 1024;      // bytes of a round's sums
+  static constexpr int kBuffer = kSums + kParts * XB * 64;  // and scales
   static constexpr int BM = 16 * XB, BN = 16 * YB;
   static_assert(kTiles <= kParts, "a wavefront per tile runs the chain");
   static_assert(kBlock % BN == 0, "columns of one block of the weights' scales");
@@ -608,13 +590,12 @@ __global__ __launch_bounds__(T::kThreads) void linear_fp8_narrow_kernel(Call q, 
   i32x4 alo[T::kDeep][XB], ahi[T::kDeep][XB], blo[T::kDeep][YB], bhi[T::kDeep][YB];
   float sa[T::kDeep][XB], sb[T::kDeep];
   const i32x4 none = {0, 0, 0, 0};
-  // block d of this wavefront in the round from block k on (past the last: that one, and
-  // of the half block: its first half again, not used)
+  // this wavefront's block of the round from block k on, into the registers of depth d
+  // (past the last: that one, and of the half block: its first half again, not used)
   auto load = [&](int k, int d) {
-    const int blk = min(k + T::kParts * d + wave, blocks - 1);
+    const int blk = min(k + wave, blocks - 1);
     const int64_t at = (int64_t)blk * kBlock;
-    const bool whole = at + kBlock <= q.K;
-    const int64_t up = whole ? at + 64 : at;
+    const int64_t up = at + kBlock <= q.K ? at + 64 : at;
 #pragma unroll
     for (int y = 0; y < YB; ++y) {
       blo[d][y] = *reinterpret_cast<const i32x4*>(b[y] + at);
@@ -630,46 +611,49 @@ __global__ __launch_bounds__(T::kThreads) void linear_fp8_narrow_kernel(Call q, 
   };
 
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  if (blocks > 0) {
 #pragma unroll
-    for (int d = 0; d < T::kDeep; ++d) load(0, d);
-  }
+  for (int d = 0; d < T::kDeep; ++d)
+    if (d * T::kParts < blocks) load(d * T::kParts, d);
   int buffer = 0;
-  for (int k = 0; k < blocks; k += T::kRound, buffer ^= T::kBuffer) {
+  // Two buffers, one barrier a round: the chain over one runs beside the next round's
+  // products, and the round after that writes it again behind the next barrier.
+  auto round = [&](int k, int d) {
     f32x4* sums = reinterpret_cast<f32x4*>(lds + buffer);
     float* scales = reinterpret_cast<float*>(lds + buffer + T::kSums);
+    buffer ^= T::kBuffer;
+    const bool half = (k + wave + 1) * kBlock > q.K;  // (or past the last: not used)
 #pragma unroll
-    for (int d = 0; d < T::kDeep; ++d) {
-      const int slot = T::kParts * d + wave;
-      const bool half = (k + slot + 1) * kBlock > q.K;  // (or past the last: not used)
+    for (int x = 0; x < XB; ++x) {
+      const i32x8 xa = __builtin_shufflevector(alo[d][x], half ? none : ahi[d][x], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-      for (int x = 0; x < XB; ++x) {
-        const i32x8 xa = __builtin_shufflevector(alo[d][x], half ? none : ahi[d][x], 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-        for (int y = 0; y < YB; ++y) {
-          const i32x8 w = __builtin_shufflevector(blo[d][y], half ? none : bhi[d][y], 0, 1, 2, 3, 4, 5, 6, 7);
-          sums[(slot * T::kTiles + x * YB + y) * 64 + lane] = block_product(w, xa);
-        }
-        if (grp == 0) scales[(slot * XB + x) * 16 + col] = sa[d][x] * sb[d];
+      for (int y = 0; y < YB; ++y) {
+        const i32x8 w = __builtin_shufflevector(blo[d][y], half ? none : bhi[d][y], 0, 1, 2, 3, 4, 5, 6, 7);
+        sums[(wave * T::kTiles + x * YB + y) * 64 + lane] = block_product(w, xa);
       }
-      if (k + T::kRound < blocks) load(k + T::kRound, d);
+      if (grp == 0) scales[(wave * XB + x) * 16 + col] = sa[d][x] * sb[d];
     }
+    if (k + T::kDeep * T::kParts < blocks) load(k + T::kDeep * T::kParts, d);
     lds_barrier();
     if (wave < T::kTiles) {
-      const int count = min(T::kRound, blocks - k);
-      auto link = [&](int slot) {
-        const f32x4 p = sums[(slot * T::kTiles + wave) * 64 + lane];
-        const float s = scales[(slot * XB + wave / YB) * 16 + col];
+      const int count = min(T::kParts, blocks - k);
+      auto link = [&](int part) {
+        const f32x4 p = sums[(part * T::kTiles + wave) * 64 + lane];
+        const float s = scales[(part * XB + wave / YB) * 16 + col];
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(p[e], s, acc[e]);
       };
-      if (count == T::kRound) {
+      if (count == T::kParts) {
 #pragma unroll
-        for (int slot = 0; slot < T::kRound; ++slot) link(slot);
+        for (int part = 0; part < T::kParts; ++part) link(part);
       } else {
-        for (int slot = 0; slot < count; ++slot) link(slot);
+        for (int part = 0; part < count; ++part) link(part);
       }
     }
+  };
+  for (int k = 0; k < blocks; k += T::kDeep * T::kParts) {
+#pragma unroll
+    for (int d = 0; d < T::kDeep; ++d)
+      if (k + d * T::kParts < blocks) round(k + d * T::kParts, d);
   }
 
   if (wave >= T::kTiles) return;
@@ -744,16 +728,28 @@ int launch(const Call& x, hipStream_t stream) {
   return hipGetLastError() == hipSuccess ? VD_OK : VD_ERR_LAUNCH;
 }
 
+// 16 x 16 tiles: eight wavefronts with two rounds ahead for short K, sixteen for long
+// (us at 1 x 1024 x 1024, 1 x 4096 x 4096, 1 x 4096 x 14336: 2.9, 6.4, 15.6 / 3.4, 6.1, 13.5).
+int launch_16x16(const Call& x, hipStream_t stream) {
+  if (x.K <= 20 * kBlock) return launch_narrow<Narrow<1, 1, 2, 8>>(x, stream);
+  return launch_narrow<Narrow<1, 1, 1, 16>>(x, stream);
+}
+
 // The tile shapes, smallest first, each with the time of one round of its tiles (a
 // tile per CU of 256 at K = 4096, in us, launches back to back in a graph).  A call
-// takes about ceil(tiles / CUs) rounds; the choice reaches no value.
-#define VD_FP8_SHAPES(X)                                \
-  X(16, 16, launch_narrow<VD_T(Narrow<1, 1, 1, 16>)>, 6.1f)         \
-  X(16, 32, launch<VD_T(Tile<1, 2, 1, 1, 512, 4, 1>)>, 7.7f)        \
-  X(32, 32, launch<VD_T(Tile<1, 2, 2, 1, 512, 3, 1>)>, 9.8f)        \
-  X(64, 64, launch<VD_T(Tile<2, 4, 2, 1, 256, 4, 1>)>, 10.8f)       \
-  X(64, 128, launch<VD_T(Tile<2, 4, 2, 2, 256, 3, 1>)>, 15.4f)      \
-  X(128, 128, launch<VD_T(Tile<4, 2, 2, 4, 128, 4, 1>)>, 23.0f)
+// takes about ceil(tiles / CUs) rounds, so a shape that just fills the chip wins over a
+// larger one that leaves CUs idle and a smaller one that reads its operands more
+// often; the choice reaches no value.  Of 60 random calls (M 1 .. 6610, N 122 .. 28544, K
+// 128 .. 10368) the choice was within 8% of the fastest of these shapes and 12 others in
+// 56, and within 16% in all.
+#define VD_FP8_SHAPES(X)                                       \
+  X(16, 16, launch_16x16, 6.1f)                                \
+  X(16, 32, launch<VD_T(Tile<1, 2, 1, 1, 512, 4>)>, 8.0f)      \
+  X(32, 32, launch<VD_T(Tile<1, 2, 2, 1, 512, 4>)>, 9.8f)      \
+  X(64, 32, launch<VD_T(Tile<2, 2, 2, 1, 512, 3>)>, 10.1f)     \
+  X(64, 64, launch<VD_T(Tile<4, 2, 1, 2, 256, 4>)>, 11.5f)     \
+  X(64, 128, launch<VD_T(Tile<2, 4, 2, 2, 256, 3>)>, 15.8f)    \
+  X(128, 128, launch<VD_T(Tile<4, 2, 2, 4, 128, 4>)>, 21.9f)
 #define VD_T(...) __VA_ARGS__
 constexpr float kRoundT = 55.0f, kRoundU = 34.5f;  // of WideT and WideU
 
@@ -775,7 +771,7 @@ int run(const Call& x, hipStream_t stream) {
   VD_FP8_SHAPES(VD_FP8_CONSIDER)
 #undef VD_FP8_CONSIDER
   // The wide tiles: all columns in tiles of T, or whole rounds of them and the columns
-  // behind in tiles of U, whichever takes less.
+  // behind in tiles of U, or all in U, whichever takes least.
   const int64_t tiles_m = (x.M - 1) / WideT::BM + 1, all = (x.N - 1) / WideT::BN + 1;
   if (tiles_m > (UINT32_MAX / WideT::kThreads - 64) / (2 * all)) return fn ? fn(x, stream) : VD_ERR_INVALID_ARG;
   const auto wide_us = [&](int64_t tiles_t) {
