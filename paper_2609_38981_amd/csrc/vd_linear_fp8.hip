@@ -49,6 +49,7 @@ namespace {
 constexpr int kBlock = 128;  // values of K per scale (one byte each)
 constexpr int kLast = 2;     // rows of tiles of a step taken together at its end
 constexpr int kGroupM = 4;   // row tiles per group of the tile order
+constexpr int64_t kMaxWideStride = INT64_C(1) << 24;  // 256 rows within 32 bits
 constexpr int64_t kMaxStride = INT64_C(1) << 29;  // 7 rows within 32 bits of a copy's first one
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -286,13 +287,15 @@ __global__ __launch_bounds__(T::kThreads) __attribute__((amdgpu_waves_per_eu(1, 
 // those: there every wavefront has read all of stage t (the copies of t + ST refill it,
 // one every kPer matrix steps) and its copies of t + 1 have landed.
 //
-// What bounds it, 4096 x 28672 x 8192 in 256 x 256 tiles: without the multiply-adds it
-// takes 743 us, without the copies 657, without both 568, all of it 800; the matrix cores
-// are busy 58% of the cycles at the 1.98 GHz that the power allows (the library's
-// unscaled product: 85% at 1.76 GHz, 610 us).  The same steps without the reads ahead 865; as
-// 32 x 32 x 64 steps 905; kLast 1, 2, 3 with the best kPer of each 803, 800, 800; copies of a
-// in a phase of their own behind a second barrier 850; 128 x 128 tiles, two workgroups
-// a CU 1075.
+// What bounds it: the power.  4096 x 28672 x 8192 in 256 x 256 tiles takes 825 us with
+// random codes and 642 (3.0 PFLOP/s) with zeros, at the same instructions (the library's
+// unscaled product: 663 and 520): the clock falls to 1.8 to 2.0 GHz, and the matrix cores are
+// busy 60% of its cycles.  Of an earlier 800 us, 743 without the multiply-adds, 657
+// without the copies, 568 without both.  Measured and not kept: no reads ahead 865; 32 x
+// 32 x 64 steps 905; three rows of tiles last 800 to 829; copies of a in a phase of their own
+// behind a second barrier 850; copies by global addresses instead of descriptors, twice
+// their instructions, 845 (at 1024 x 6144 x 4096, short of the power limit, 58.3 against
+// 54.3); 128 x 128 tiles, two workgroups a CU, 1060.
 // ---------------------------------------------------------------------------
 template <int WM_, int WN_, int XB_, int YB_, int ST_, int kPer_>
 struct Wide {
@@ -305,9 +308,11 @@ struct Wide {
   static constexpr int kLds = ST * kStage;
   static constexpr int kCopiesA = kTileA / 1024 / kWaves, kCopiesB = kTileB / 1024 / kWaves;
   static constexpr int kCopies = kCopiesA + kCopiesB;  // per wavefront and step
+  static constexpr int kUnits = kCopies / 2 + 1;       // pairs of them, and the scales
   static constexpr int kScaleWaves = (BM + 63) / 64;
   static_assert(kCopiesA * kWaves * 1024 == kTileA && kCopiesB * kWaves * 1024 == kTileB, "copy split");
-  static_assert(kCopies * kPer < XB * YB, "a step's copies are issued before its barrier");
+  static_assert(kCopiesA % 2 == 0 && kCopiesB % 2 == 0, "copies of one matrix in pairs");
+  static_assert((kUnits - 1) * kPer < XB * YB, "a step's copies are issued before its barrier");
   static_assert(kScaleWaves < kWaves, "a wavefront for the weights' scales");
   static_assert(kBlock % (16 * YB) == 0 && YB % 4 == 0, "a wavefront's columns lie in one block of the weights' scales");
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
@@ -319,54 +324,55 @@ __device__ __forceinline__ void wide_tile(const Call& q, int64_t m0, int n0) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int wave = uni(threadIdx.x >> 6);
   const int lane = __lane_id();
-  // Copies: as in the kernel above; a wavefront's copy j carries 8 rows of a (j <
-  // kCopiesA) or b.  Rows past the last read the end of the last one's block
-  // instead (limit), in bounds and never stored.
-  const uint8_t* src[T::kCopies];
-  uint32_t limit[T::kCopies];
-#pragma unroll
-  for (int j = 0; j < T::kCopies; ++j) {
-    const bool is_a = j < T::kCopiesA;
-    const int64_t r0 = is_a ? m0 + 8 * (wave * T::kCopiesA + j) : n0 + 8 * (wave * T::kCopiesB + j - T::kCopiesA);
-    const int64_t last = (is_a ? q.M : q.N) - 1, ld = is_a ? q.lda : q.ldb;
-    const int64_t r = r0 < last ? r0 : last;
-    const int64_t below = last - r < 7 ? last - r : 7;
-    src[j] = (is_a ? q.a : q.b) + r * ld;
-    limit[j] = (uint32_t)(below * ld) + 112;
-  }
+  // Copies: as in the kernel above, through descriptors of the tile's rows of a and of b
+  // that move along K; a wavefront's copies j < kCopiesA carry 8 rows of a each, the
+  // others of b, two at a time.  Rows past the last are out of range: zeros, never
+  // stored; a half block's bytes past K are whatever lies there, never used.
+  const int blocks = (q.K + kBlock - 1) / kBlock;
   const uint32_t ck = 16 * ((lane % 8) ^ (lane / 8));
   const uint32_t off_a = (uint32_t)((lane / 8) * q.lda) + ck, off_b = (uint32_t)((lane / 8) * q.ldb) + ck;
-  const int blocks = (q.K + kBlock - 1) / kBlock;
-  const float* scale_src;
-  int64_t scale_step;
-  if (wave < T::kScaleWaves) {
-    const int64_t m = m0 + 64 * wave + lane;
-    scale_src = q.as + (m < q.M ? m : q.M - 1) * q.as_row;
-    scale_step = q.as_blk;
-  } else {
-    // (lanes past the tile's blocks repeat its last one: few lines)
-    const int end = (q.N - 1) / kBlock, at = n0 / kBlock + min(lane, (T::BN - 1) / kBlock);
-    scale_src = q.bs + (int64_t)(at < end ? at : end) * q.bs_row;
-    scale_step = q.bs_blk;
-  }
+  const auto bytes_of = [&](int64_t first, int64_t rows, int64_t ld, int tile) {
+    const int64_t last = rows - 1 - first < tile - 1 ? rows - 1 - first : tile - 1;
+    return (uint32_t)(last * ld + q.K);
+  };
+  uint64_t at_a = (uint64_t)(q.a + m0 * q.lda), at_b = (uint64_t)(q.b + n0 * q.ldb);
+  uint32_t bytes_a = bytes_of(m0, q.M, q.lda, T::BM), bytes_b = bytes_of(n0, q.N, q.ldb, T::BN);
+  const uint32_t row_a = 8 * T::kCopiesA * wave, row_b = 8 * T::kCopiesB * wave;
+  // (lanes past the tile's blocks of b repeat its last one: few lines)
+  const bool of_a = wave < T::kScaleWaves;
+  const int64_t sm = min(m0 + 64 * wave + lane, q.M - 1);
+  const int64_t sn = min(n0 / kBlock + min(lane, (T::BN - 1) / kBlock), (q.N - 1) / kBlock);
+  const float* scale_a = q.as + sm * q.as_row;
+  const float* scale_b = q.bs + sn * q.bs_row;
+  const float* scale_src = of_a ? scale_a : scale_b;
+  const int64_t scale_step = of_a ? q.as_blk : q.bs_blk;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const uint32_t dst_a = lds0 + 1024 * T::kCopiesA * wave, dst_b = lds0 + T::kTileA + 1024 * T::kCopiesB * wave;
   const uint32_t dst_scale = lds0 + T::kTileA + T::kTileB + 256 * wave;
-  // copy j of step t (the last one: scales) into its stage (from byte st on); past K: the
-  // last block again
-  auto fetch = [&](int t, int st, int j) {
-    const int blk = min(t, blocks - 1);
-    if (j < T::kCopies) {
-      // (a half block: its bytes past K are those before it, never used)
-      const bool half = blk * kBlock + kBlock > q.K;
-      const uint32_t off = j < T::kCopiesA ? off_a : off_b;
-      const uint32_t o = half ? off - (ck & 64) : off, lim = half ? limit[j] - 64 : limit[j];
-      const uint32_t at = j < T::kCopiesA ? dst_a + st + 1024 * j
-                                          : dst_b + st + 1024 * (j - T::kCopiesA);
-      lds_dma16_at(src[j] + (int64_t)blk * kBlock, min(o, lim), uni((int)at));
+  // unit u of the copies of the block that the descriptors stand at, into the stage from
+  // byte st on: two copies, or (the last one) the scales
+  auto fetch = [&](int st, int u) {
+    if (2 * u < T::kCopiesA) {
+      const uint32_t r = row_a + 16 * u;
+      lds_dma16_pair(buffer_of(at_a, bytes_a), off_a, (uint32_t)(r * q.lda), (uint32_t)((r + 8) * q.lda),
+                     uni((int)(dst_a + st + 2048 * u)));
+    } else if (2 * u < T::kCopies) {
+      const uint32_t r = row_b + 16 * u - 8 * T::kCopiesA;
+      lds_dma16_pair(buffer_of(at_b, bytes_b), off_b, (uint32_t)(r * q.ldb), (uint32_t)((r + 8) * q.ldb),
+                     uni((int)(dst_b + st + 2048 * u - 1024 * T::kCopiesA)));
     } else {
-      lds_dma4(scale_src + blk * scale_step, uni((int)(dst_scale + st)));
+      lds_dma4(scale_src, uni((int)(dst_scale + st)));
     }
+  };
+  int left = blocks - 1;  // blocks behind the one the descriptors stand at
+  auto advance = [&] {
+    const int by = left > 0 ? kBlock : 0;
+    at_a += by;
+    at_b += by;
+    bytes_a -= by;
+    bytes_b -= by;
+    scale_src += left > 0 ? scale_step : 0;
+    --left;
   };
 
   const int wm = 16 * XB * (wave / T::WN), wn = 16 * YB * (wave % T::WN);
@@ -411,7 +417,7 @@ __device__ __forceinline__ void wide_tile(const Call& q, int64_t m0, int n0) {
   auto read_w = [&](int st, int y) { wv[y % 4] = operand(b0 + st, 16 * y * kBlock); };
   auto read_bs = [&](int st) { bs = *reinterpret_cast<const float*>(t0 + st); };
   // st, next: the stages of this step and of the next one; before: of the step ST - 1 ahead
-  auto step = [&](int t, int st, int next, int before) {
+  auto step = [&](int st, int next, int before) {
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       const int x = x_of(i), y = y_of(i);
@@ -426,6 +432,7 @@ __device__ __forceinline__ void wide_tile(const Call& q, int64_t m0, int n0) {
       if (i == XB * kFirst) {
         wait_vmcnt<(ST - 2) * (T::kCopies + 1)>();
         lds_barrier();
+        advance();
         read_w(next, 0);
         read_bs(next);
       }
@@ -438,25 +445,28 @@ __device__ __forceinline__ void wide_tile(const Call& q, int64_t m0, int n0) {
       p[i % 4] = block_product(wv[y % 4], xa[x]);
       if (y + 1 == YB) read_x(next, x);
 #pragma unroll
-      for (int j = 0; j <= T::kCopies; ++j) {
-        // copies of t + ST into this stage from the barrier on, one every kPer matrix
-        // steps, the last of them in the next block (into the stage before it)
-        const int at = XB * kFirst + j * T::kPer;
-        if (at == i) fetch(t + ST, st, j);
-        if (at - kSteps == i) fetch(t + ST - 1, before, j);
+      for (int u = 0; u < T::kUnits; ++u) {
+        // copies of the step ST ahead into this stage from the barrier on, a unit every kPer
+        // matrix steps, the last of them in the next step (into the stage before it)
+        const int at = XB * kFirst + u * T::kPer;
+        if (at == i) fetch(st, u);
+        if (at - kSteps == i) fetch(before, u);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
 
   if (blocks > 0) {
-    constexpr int in_step = (kSteps - XB * kFirst - 1) / T::kPer + 1;  // copies of a step issued within it
-    constexpr int early = in_step < T::kCopies + 1 ? in_step : T::kCopies + 1;
+    constexpr int in_step = (kSteps - XB * kFirst - 1) / T::kPer + 1;  // units of a step issued within it
+    constexpr int early = in_step < T::kUnits ? in_step : T::kUnits;
+    constexpr int early_copies = early < T::kUnits ? 2 * early : T::kCopies + 1;
 #pragma unroll
-    for (int t = 0; t < ST; ++t)
+    for (int t = 0; t < ST; ++t) {
+      if (t > 0) advance();
 #pragma unroll
-      for (int j = 0; j < (t < ST - 1 ? T::kCopies + 1 : early); ++j) fetch(t, t * T::kStage, j);
-    wait_vmcnt<(ST - 2) * (T::kCopies + 1) + early>();
+      for (int u = 0; u < (t < ST - 1 ? T::kUnits : early); ++u) fetch(t * T::kStage, u);
+    }
+    wait_vmcnt<(ST - 2) * (T::kCopies + 1) + early_copies>();
     lds_barrier();
     read_w(0, 0);
     read_bs(0);
@@ -466,7 +476,7 @@ __device__ __forceinline__ void wide_tile(const Call& q, int64_t m0, int n0) {
     int st = 0, before = (ST - 1) * T::kStage;
     for (int t = 0; t < full; ++t) {
       const int next = st == (ST - 1) * T::kStage ? 0 : st + T::kStage;
-      step(t, st, next, before);
+      step(st, next, before);
       before = st;
       st = next;
     }
@@ -527,8 +537,8 @@ __device__ __forceinline__ void wide_tile(const Call& q, int64_t m0, int n0) {
 // The call's first columns in tiles of T, the others in tiles of U: the workgroups
 // before `first_u` take the former.  Whole rounds of T and the rest in U: 4096 x 6144 x
 // 4096 109 us in a graph, T alone 124, U alone 121.
-using WideT = Wide<4, 2, 4, 8, 2, 2>;  // 256 x 256
-using WideU = Wide<4, 2, 4, 4, 3, 2>;  // 256 x 128
+using WideT = Wide<4, 2, 4, 8, 2, 3>;  // 256 x 256
+using WideU = Wide<4, 2, 4, 4, 3, 4>;  // 256 x 128
 
 __global__ __launch_bounds__(WideT::kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void linear_fp8_wide_kernel(
     Call q, int tiles_m, int tiles_t, int tiles_u, uint32_t first_u, int xcd_shift) {
@@ -770,6 +780,8 @@ int run(const Call& x, hipStream_t stream) {
 #define VD_FP8_CONSIDER(bm, bn, f, us) consider(bm, bn, &f, us);
   VD_FP8_SHAPES(VD_FP8_CONSIDER)
 #undef VD_FP8_CONSIDER
+  // (the wide tiles' rows lie within 32 bits of a descriptor's base)
+  if (fn && (x.lda >= kMaxWideStride || x.ldb >= kMaxWideStride)) return fn(x, stream);
   // The wide tiles: all columns in tiles of T, or whole rounds of them and the columns
   // behind in tiles of U, or all in U, whichever takes least.
   const int64_t tiles_m = (x.M - 1) / WideT::BM + 1, all = (x.N - 1) / WideT::BN + 1;

@@ -97,9 +97,9 @@ def test_tile_shapes(m, n, ks):
         O.same_bits(V.linear_fp8(a, a_s, b[c:], b_s[c // 128:]), full[:, c:], k)
 
 
-@pytest.mark.parametrize("m", [1, 20, 70, 300])
-def test_strides(m):
-    n, k = 333, 448
+@pytest.mark.parametrize("m,n", [(1, 333), (20, 333), (70, 333), (300, 333), (700, 6000), (4095, 4090)])
+def test_strides(m, n):
+    k, nb = 448, -(-n // 128)
     x = a, a_s, b, b_s = _draw(m, m, n, k)
     full = V.linear_fp8(*x)
     nan = torch.full((max(m, n), k + 48), 0x7F, dtype=torch.uint8, device="cuda").view(V.E4M3)
@@ -108,7 +108,7 @@ def test_strides(m):
     b2.copy_(b)
     s2 = torch.full((m, 9), float("nan"), device="cuda")[:, 1::2][:, :4]
     s2.copy_(a_s)
-    t2 = torch.full((5, 7), float("nan"), device="cuda").t()[:3, 1:5]
+    t2 = torch.full((5, nb + 4), float("nan"), device="cuda").t()[:nb, 1:5]
     t2.copy_(b_s)
     out = torch.full((m + 2, n + 8), 7.0, dtype=torch.bfloat16, device="cuda")
     V.linear_fp8(a2, s2, b2, t2, out=out[1:m + 1, 3:3 + n])
@@ -116,8 +116,8 @@ def test_strides(m):
     out[1:m + 1, 3:3 + n] = 7.0
     assert (out == 7).all()  # nothing around the rows and columns was written
     # one scale for all rows, and for all blocks
-    O.same_bits(V.linear_fp8(a, a_s[:1, :1].expand(m, 4), b, b_s[:1, :1].expand(3, 4)),
-                V.linear_fp8(a, a_s[:1, :1].repeat(m, 4), b, b_s[:1, :1].repeat(3, 4)))
+    O.same_bits(V.linear_fp8(a, a_s[:1, :1].expand(m, 4), b, b_s[:1, :1].expand(nb, 4)),
+                V.linear_fp8(a, a_s[:1, :1].repeat(m, 4), b, b_s[:1, :1].repeat(nb, 4)))
 
 
 @pytest.mark.parametrize("m", [2, 40, 70, 300])
@@ -212,6 +212,21 @@ def test_offsets_past_32_bits():
     c = wide[:, :n]
     V.linear_fp8(a[:70], a_s[:70], b, b_s, out=c)
     O.same_bits(c, V.linear_fp8(a[:70], a_s[:70], b, b_s))
+
+
+def test_rows_far_apart():
+    """Row strides up to 2^24 (the wide tiles' limit is below it), and one past it."""
+    m, n, k = 700, 6000, 192
+    a, a_s, b, b_s = _draw(3, m, n, k)
+    want = V.linear_fp8(a, a_s, b, b_s)
+    big = torch.empty((m * 2**24 // 2**20 + 1, 2**20), dtype=torch.uint8, device="cuda").view(-1)  # 11.7 GB
+    for ld in (2**24 - 16, 2**24):
+        far = big[:m * ld].view(m, ld)[:, :k].view(V.E4M3)
+        far.copy_(a)
+        O.same_bits(V.linear_fp8(far, a_s, b, b_s), want, ld)
+        far = big[:600 * ld].view(600, ld)[:, :k].view(V.E4M3)
+        far.copy_(b[:600])
+        O.same_bits(V.linear_fp8(a, a_s, far, b_s[:5]), want[:, :600], ld)
 
 
 def test_wrapper_refuses():
