@@ -20,9 +20,10 @@
 // wavefronts in ascending order -- whose shape follows K alone, and a group's
 // maximum is exact.
 //
-// What bounds them: HBM with many rows -- 8192 x 4096 with the residual into 8 bits 41 us
-// (5.7 TB/s read and written; a large copy moves 5.0), 4096 x 14336 with the gate 58 us (5.0)
-// -- and with few the launch (2.2 us) and one chain of load, sum and store: 1 x 4096 2.9
+// What bounds them: HBM with many rows -- 8192 x 4096 with the residual into 8 bits 39.4
+// us (6.0 TB/s read and written; a large copy moves 5.0), 4096 x 14336 with the gate 55.9
+// (5.3); with neighbouring rows on different dies, whose caches then each write a part of
+// a line of scales, 41.3 and 58.5 -- and with few the launch (2.2 us) and one chain of load, sum and store: 1 x 4096 2.9
 // us, 77 x 8192 with the residual into 8 bits 4.1, 64 x 4096 rows in 8 bits 2.5.
 #include <hip/hip_runtime.h>
 
@@ -41,6 +42,8 @@ namespace {
 constexpr int kGroup = 128;       // values per scale
 constexpr int kMaxNormK = 32768;  // 1024 threads of 4 vectors of 8
 constexpr int64_t kMaxGroups = INT64_C(1) << 27;  // of a launch: its threads are counted in 32 bits
+constexpr int kRun = 32;           // neighbouring rows of a die: a 128-byte line of scales
+constexpr int kTileRows = 32;      // (8, 16, 32, 64: 56.6, 56.3, 55.9, 57.4 us at 4096 x 14336 with the gate)
 constexpr float kMinTop = 0x1p-117f;
 constexpr float kPer448 = 1.0f / 448.0f;
 
@@ -98,7 +101,18 @@ struct NormArgs {
   int64_t ldx, ldr, lds, ldo, s_row, s_blk, M;
   int K;
   float eps;
+  int64_t slots;       // rows, or whole runs of them on every die
+  int run, xcd_shift;  // rows of a run (0: the rows in order)
 };
+
+// The row of slot i.  Workgroup b runs on die b mod the die count: there it takes runs of
+// neighbouring rows, so that their scales, which lie side by side, meet in one L2 line
+// before they leave it.
+__device__ __forceinline__ int64_t row_of(int64_t i, const NormArgs& a) {
+  if (a.run == 0) return i;
+  const int64_t j = i >> a.xcd_shift, x = i & ((1 << a.xcd_shift) - 1);
+  return ((j / a.run << a.xcd_shift) + x) * a.run + j % a.run;
+}
 
 // A workgroup per row (rows strided by the grid), V vectors of 8 values a lane:
 // vector v of thread t holds values 8 (v T + t) .. + 7 of T threads.
@@ -113,7 +127,9 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
   for (int v = 0; v < V; ++v)
     if (v * threads + tid < vecs) wv[v] = *reinterpret_cast<const u16x8*>(a.w + 8 * (v * threads + tid));
   int parity = 0;
-  for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x, parity ^= 1) {
+  for (int64_t i = blockIdx.x; i < a.slots; i += gridDim.x) {
+    const int64_t row = row_of(i, a);
+    if (row >= a.M) continue;
     float h[V][8];
     float ss = 0.0f;
 #pragma unroll
@@ -139,6 +155,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
       __syncthreads();
       ss = part[parity][0];
       for (int w = 1; w < waves; ++w) ss += part[parity][w];
+      parity ^= 1;
     }
     const float r = 1.0f / __builtin_sqrtf(ss / (float)a.K + a.eps);
 #pragma unroll
@@ -173,7 +190,8 @@ struct RowArgs {
   uint8_t* out;
   float* scales;
   int64_t ldx, ldg, ldo, s_row, s_blk;
-  uint32_t groups, per_row;  // groups of all rows and of one
+  int64_t M;
+  uint32_t per_row;  // groups of a row
   int K;
 };
 
@@ -193,22 +211,33 @@ __device__ __forceinline__ float silu(float g) {
   return (g < 0.0f ? g * t : g) * r;
 }
 
-// 16 lanes per group of 128 values, groups in row order; a workgroup takes U times 16 of
-// them, all loads before the arithmetic.
-template <bool GATE, int U>
+// 16 lanes per group of 128 values.  Few rows: a workgroup takes 16 groups in row order.
+// Many (TILE): 4 groups a lane, all loads before the arithmetic, a tile of kTileRows rows x
+// 64 / kTileRows groups a workgroup, so that the scales of neighbouring rows, which lie side
+// by side, meet in one L2 line before they leave it.
+template <bool GATE, bool TILE>
 __global__ __launch_bounds__(256) void quantize_kernel(RowArgs a) {
-  const int lane16 = threadIdx.x & 15;
-  const uint32_t u0 = blockIdx.x * (16u * U) + (threadIdx.x >> 4);
+  constexpr int U = TILE ? 4 : 1;
+  const int lane16 = threadIdx.x & 15, unit = threadIdx.x >> 4;
   u16x8 xv[U], gv[U];
-  uint32_t row[U], g[U];
+  int64_t row[U];
+  uint32_t g[U];
   bool in[U];
 #pragma unroll
   for (int j = 0; j < U; ++j) {
-    const uint32_t u = u0 + 16u * j;
-    row[j] = u / a.per_row;
-    g[j] = u - row[j] * a.per_row;
+    if (TILE) {
+      constexpr int kCols = 64 / kTileRows;
+      const uint32_t tiles = (a.per_row - 1) / kCols + 1;
+      const uint32_t v = unit + 16 * j;  // of the tile's 64 groups, a row's beside each other
+      row[j] = (int64_t)(blockIdx.x / tiles) * kTileRows + v / kCols;
+      g[j] = blockIdx.x % tiles * kCols + v % kCols;
+    } else {
+      const uint32_t u = blockIdx.x * 16u + unit;
+      row[j] = u / a.per_row;
+      g[j] = u % a.per_row;
+    }
     const int k = (int)g[j] * kGroup + 8 * lane16;
-    in[j] = u < a.groups && k < a.K;
+    in[j] = row[j] < a.M && k < a.K;
     xv[j] = gv[j] = u16x8{};
     if (in[j]) {
       xv[j] = *reinterpret_cast<const u16x8*>(a.x + row[j] * a.ldx + k);
@@ -257,13 +286,21 @@ int check_norm(const NormArgs& a, int64_t K) {
 }
 
 template <bool FP8>
-int launch_norm(const NormArgs& a, hipStream_t stream) {
+int launch_norm(NormArgs a, hipStream_t stream) {
   // 2 vectors a lane (1 for rows of one wavefront's vectors, 4 for rows of more
   // than 16 wavefronts' pairs): by K alone, the sum's order is its
   const int per_lane = a.K <= 512 ? 1 : a.K <= 16384 ? 2 : 4;
   const int waves = (a.K + 512 * per_lane - 1) / (512 * per_lane);
   const dim3 block(64 * waves);
-  const dim3 grid((unsigned)std::min<int64_t>(a.M, 1 << 16));
+  // Runs of 32 rows (a line of scales) where the dies have several each
+  const Geometry geo = device_geometry();
+  a.slots = a.M;
+  if (FP8 && a.M >= 4 * kRun * geo.xcds) {
+    a.run = kRun;
+    a.xcd_shift = geo.xcd_shift;
+    a.slots = (a.M + kRun * geo.xcds - 1) / (kRun * geo.xcds) * (kRun * geo.xcds);
+  }
+  const dim3 grid((unsigned)std::min<int64_t>(a.slots, 1 << 16));
 #define VD_NORM(V)                                                                        \
   if (a.res)                                                                              \
     hipLaunchKernelGGL((norm_kernel<V, true, FP8>), grid, block, 0, stream, a);           \
@@ -289,7 +326,7 @@ int vd_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ldr, co
                hipStream_t stream) {
   const NormArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(residual),
                    static_cast<const uint16_t*>(weight), static_cast<uint16_t*>(sum), out, nullptr,
-                   ldx, ldr, lds, ldo, 0, 0, M, K, eps};
+                   ldx, ldr, lds, ldo, 0, 0, M, K, eps, 0, 0, 0};
   const int rc = check_norm(a, K);
   if (rc != VD_OK || M == 0 || K == 0) return rc;
   if (bad_rows(out, ldo, K)) return VD_ERR_INVALID_ARG;
@@ -302,7 +339,7 @@ int vd_rmsnorm_fp8(const void* x, int64_t ldx, const void* residual, int64_t ldr
                    hipStream_t stream) {
   const NormArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(residual),
                    static_cast<const uint16_t*>(weight), static_cast<uint16_t*>(sum), out, scales,
-                   ldx, ldr, lds, ldo, s_row, s_blk, M, K, eps};
+                   ldx, ldr, lds, ldo, s_row, s_blk, M, K, eps, 0, 0, 0};
   const int rc = check_norm(a, K);
   if (rc != VD_OK || M == 0 || K == 0) return rc;
   if (bad_codes(out, ldo, scales, s_row, s_blk, M, K)) return VD_ERR_INVALID_ARG;
@@ -321,19 +358,20 @@ int vd_quantize_fp8(const void* x, int64_t ldx, const void* gate, int64_t ldg, v
     return VD_ERR_INVALID_ARG;
   const RowArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(gate),
                   static_cast<uint8_t*>(out), scales, ldx, ldg, ldo, s_row, s_blk,
-                  (uint32_t)(M * per_row), (uint32_t)per_row, K};
-  // 4 groups a lane where that leaves several workgroups per CU, else one
-  const bool many = a.groups >= 16u * 4 * 4 * device_geometry().cus;
-  const dim3 grid((a.groups - 1) / (many ? 64 : 16) + 1);
-#define VD_ROWS(GATE, U) hipLaunchKernelGGL((quantize_kernel<GATE, U>), grid, dim3(256), 0, stream, a)
+                  M, (uint32_t)per_row, K};
+  // tiles where they leave several workgroups per CU
+  const uint32_t tiles = (uint32_t)(((M - 1) / kTileRows + 1) * ((per_row - 1) / (64 / kTileRows) + 1));
+  const bool many = tiles >= 4u * device_geometry().cus;
+  const dim3 grid(many ? tiles : (uint32_t)((M * per_row - 1) / 16 + 1));
+#define VD_ROWS(GATE, TILE) hipLaunchKernelGGL((quantize_kernel<GATE, TILE>), grid, dim3(256), 0, stream, a)
   if (gate && many)
-    VD_ROWS(true, 4);
+    VD_ROWS(true, true);
   else if (gate)
-    VD_ROWS(true, 1);
+    VD_ROWS(true, false);
   else if (many)
-    VD_ROWS(false, 4);
+    VD_ROWS(false, true);
   else
-    VD_ROWS(false, 1);
+    VD_ROWS(false, false);
 #undef VD_ROWS
   return hipGetLastError() == hipSuccess ? VD_OK : VD_ERR_LAUNCH;
 }

@@ -116,6 +116,27 @@ def test_rows_do_not_depend_on_the_call(k):
     assert (sc[:, 0] == 0).all() and (sc[:, 1 - (-k // 128):] == 0).all()
 
 
+@pytest.mark.parametrize("m,k", [(1024, 4104), (2077, 4104), (1025, 128), (40000, 200)])
+def test_many_rows(m, k):
+    """Calls whose rows go to the dies in runs and whose groups in tiles: every row has the bits
+    of calls of 100 rows, and nothing behind the last row or group is written."""
+    x, r, w = _rows(k, m, k), _rows(k + 1, m, k, scale=3.0), _weight(1, k)
+    kb = -(-k // 128)
+    for f in (lambda a, b, **o: V.rmsnorm_fp8(a, w, EPS, residual=b, **o), lambda a, b, **o: V.quantize_fp8(a, **o),
+              lambda a, b, **o: V.quantize_fp8(a, gate=b, **o)):
+        codes = torch.full((m + 40, k + 8), 1.0, device="cuda").to(V.E4M3)
+        scales = torch.full((kb + 1, m + 40), -1.0, device="cuda").t()
+        got = f(x, r, out=codes[:m, :k], scales=scales[:m, :kb])
+        for lo in sorted({0, 31, m // 2, m - 100}):
+            part = f(x[lo:lo + 100], r[lo:lo + 100])
+            for p, whole in zip(part, got):
+                O.same_bits(p, whole[lo:lo + 100], lo)
+        all_rows = torch.cat([f(x[i:i + 500], r[i:i + 500])[1] for i in range(0, m, 500)])
+        O.same_bits(all_rows, got[1])
+        assert (codes[m:].float() == 1).all() and (codes[:, k:].float() == 1).all()
+        assert (scales[m:] == -1).all() and (scales[:, kb:] == -1).all()
+
+
 def test_not_finite_and_extreme_values():
     k = 264
     w = torch.ones(k, dtype=torch.bfloat16, device="cuda")
