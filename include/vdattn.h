@@ -307,7 +307,8 @@ int vd_kv_write(const vd_attn* h, const void* k_new, const void* v_new,
  *   the rows behind the last request and where the page id is outside [0, num_pages)
  *   status[r]: 0, or the bit mask of why the request is refused:
  *     1  s < 0, c < 0 or n > 2^31 - 1;      2  ceil(n / 16) > pt_stride;
- *     4  the free list has too few pages;   8  its rows end past total_q_tokens.
+ *     4  the free list ends before its pages (it and every later request that needs a page);
+ *     8  its rows end past total_q_tokens.
  * A refused request takes no page, its table row is left as it was, its context_lens is 0 (the
  * attention skips it) and its rows' slots are -1 (the KV write skips them).  A request without
  * new tokens (s = 0) is not refused; the attention skips it.
@@ -316,7 +317,7 @@ int vd_kv_write(const vd_attn* h, const void* k_new, const void* v_new,
  * VD_ERR_INVALID_ARG).  One launch on `stream`, no workspace; it may be captured, and a replay
  * reads the lengths that are there then. */
 typedef struct {
-  int32_t num_seqs;            /* B >= 0 */
+  int32_t num_seqs;            /* B, 0 .. 2^31 - 4097 */
   int64_t total_q_tokens;      /* rows of slot_mapping, 0 .. 2^31 - 4097; may be more than sum s */
   const int32_t* q_lens;       /* [B] */
   const int32_t* cached_lens;  /* [B] */

@@ -122,6 +122,24 @@ def test_slots_past_32_bits():
     assert want["slot_mapping"].tolist() == [(pages - 2) * 16 + 15, (pages - 1) * 16, (2**28 + 3) * 16 + 8]
 
 
+def test_table_past_32_bits():
+    """A table of 2.4e9 entries: the last requests' pages are where they belong."""
+    B, stride = 9200, 2**18
+    table = torch.full((B, stride), FILL, dtype=torch.int32, device="cuda")
+    c = torch.zeros(B, dtype=torch.int32, device="cuda")
+    c[B - 1] = 16 * (stride - 2)
+    table[B - 1, stride - 3] = 5
+    q = torch.ones(B, dtype=torch.int32, device="cuda")
+    q[B - 1] = 20
+    free = torch.arange(10, B + 20, dtype=torch.int32, device="cuda")
+    m = V.map_pages(q, c, free, table, B + 30, B + 19)
+    assert (m.status == 0).all() and int(m.pages_used) == B + 1
+    assert table[B - 1, stride - 2:].tolist() == [10 + B - 1, 10 + B]
+    assert torch.equal(table[:B - 1, 0], free[:B - 1]) and (table[B - 2, 1:] == FILL).all()
+    assert m.slot_mapping[B - 1:].tolist() == [(10 + B - 1) * 16 + i for i in range(16)] + [
+        (10 + B) * 16 + i for i in range(4)]
+
+
 def test_wrapper_refuses():
     i = _i32([1, 2])
     t = _i32([[0], [1]])
