@@ -106,7 +106,7 @@ def main() -> int:
             "LD_PRELOAD": clang_asan_runtime(),
             "ASAN_OPTIONS": "detect_leaks=0:abort_on_error=1",
             "UBSAN_OPTIONS": "print_stacktrace=1:halt_on_error=1"},
-            ["tests/test_abi_cpu.py"])
+            ["tests/test_abi_cpu.py", "tests/test_ops_cpu.py"])
     print("sanitizer runs: %s" % ("all clean" if ok else "FAILED"), flush=True)
     return 0 if ok else 1
 

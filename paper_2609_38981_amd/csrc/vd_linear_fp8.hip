@@ -693,21 +693,35 @@ int64_t grid_blocks(const Call& x, int bm, int bn, int threads, int xcds) {
   return blocks * threads <= UINT32_MAX ? blocks : -1;
 }
 
-// `tiles_t` column tiles of WideT, and WideU's for the columns behind them.
+// The workgroups of a call with `tiles_t` column tiles of WideT and WideU's for the columns
+// behind them, each kind's a multiple of the dies.
+struct WideGrid {
+  int64_t tiles_m, tiles_u, first_u, blocks;
+  WideGrid(const Call& x, int64_t tiles_t, const Geometry& geo) {
+    const int64_t rest = x.N - tiles_t * WideT::BN;
+    tiles_m = (x.M - 1) / WideT::BM + 1;
+    tiles_u = rest > 0 ? (rest - 1) / WideU::BN + 1 : 0;
+    const auto padded = [&](int64_t tiles) { return (tiles + geo.xcds - 1) / geo.xcds * geo.xcds; };
+    if (tiles_m > UINT32_MAX) {  // (and no product below passes 64 bits)
+      first_u = blocks = INT64_MAX;
+      return;
+    }
+    first_u = padded(tiles_m * tiles_t);
+    blocks = first_u + padded(tiles_m * tiles_u);
+  }
+  bool fits() const { return blocks <= UINT32_MAX / WideT::kThreads; }
+};
+
 int launch_wide(const Call& x, int64_t tiles_t, hipStream_t stream) {
   const Geometry geo = device_geometry();
-  const int64_t tiles_m = (x.M - 1) / WideT::BM + 1;
-  const int64_t rest = x.N - tiles_t * WideT::BN;
-  const int64_t tiles_u = rest > 0 ? (rest - 1) / WideU::BN + 1 : 0;
-  const int64_t first_u = (tiles_m * tiles_t + geo.xcds - 1) / geo.xcds * geo.xcds;
-  const int64_t blocks = first_u + (tiles_m * tiles_u + geo.xcds - 1) / geo.xcds * geo.xcds;
-  if (blocks * WideT::kThreads > UINT32_MAX) return VD_ERR_INVALID_ARG;
+  const WideGrid g(x, tiles_t, geo);
+  if (!g.fits()) return VD_ERR_INVALID_ARG;
   constexpr int lds = WideT::kLds > WideU::kLds ? WideT::kLds : WideU::kLds;
   static std::atomic<unsigned char> lds_set[kMaxDevices];
   if (set_lds_limit(reinterpret_cast<const void*>(&linear_fp8_wide_kernel), lds, lds_set) != hipSuccess)
     return VD_ERR_LAUNCH;
-  hipLaunchKernelGGL(linear_fp8_wide_kernel, dim3((unsigned)blocks), dim3(WideT::kThreads), lds, stream,
-                     x, (int)tiles_m, (int)tiles_t, (int)tiles_u, (uint32_t)first_u, geo.xcd_shift);
+  hipLaunchKernelGGL(linear_fp8_wide_kernel, dim3((unsigned)g.blocks), dim3(WideT::kThreads), lds, stream,
+                     x, (int)g.tiles_m, (int)tiles_t, (int)g.tiles_u, (uint32_t)g.first_u, geo.xcd_shift);
   return hipGetLastError() == hipSuccess ? VD_OK : VD_ERR_LAUNCH;
 }
 
@@ -745,21 +759,21 @@ int launch_16x16(const Call& x, hipStream_t stream) {
   return launch_narrow<Narrow<1, 1, 1, 16>>(x, stream);
 }
 
-// The tile shapes, smallest first, each with the time of one round of its tiles (a
-// tile per CU of 256 at K = 4096, in us, launches back to back in a graph).  A call
+// The tile shapes, smallest first, each with its threads and the time of one round of its
+// tiles (a tile per CU of 256 at K = 4096, in us, launches back to back in a graph).  A call
 // takes about ceil(tiles / CUs) rounds, so a shape that just fills the chip wins over a
 // larger one that leaves CUs idle and a smaller one that reads its operands more
 // often; the choice reaches no value.  Of 60 random calls (M 1 .. 6610, N 122 .. 28544, K
 // 128 .. 10368) the choice was within 8% of the fastest of these shapes and 12 others in
 // 56, and within 16% in all.
-#define VD_FP8_SHAPES(X)                                       \
-  X(16, 16, launch_16x16, 6.1f)                                \
-  X(16, 32, launch<VD_T(Tile<1, 2, 1, 1, 512, 4>)>, 8.0f)      \
-  X(32, 32, launch<VD_T(Tile<1, 2, 2, 1, 512, 4>)>, 9.8f)      \
-  X(64, 32, launch<VD_T(Tile<2, 2, 2, 1, 512, 3>)>, 10.1f)     \
-  X(64, 64, launch<VD_T(Tile<4, 2, 1, 2, 256, 4>)>, 11.5f)     \
-  X(64, 128, launch<VD_T(Tile<2, 4, 2, 2, 256, 3>)>, 15.8f)    \
-  X(128, 128, launch<VD_T(Tile<4, 2, 2, 4, 128, 4>)>, 21.9f)
+#define VD_FP8_SHAPES(X)                                                \
+  X(16, 16, 1024, launch_16x16, 6.1f)                                   \
+  X(16, 32, 128, launch<VD_T(Tile<1, 2, 1, 1, 512, 4>)>, 8.0f)          \
+  X(32, 32, 128, launch<VD_T(Tile<1, 2, 2, 1, 512, 4>)>, 9.8f)          \
+  X(64, 32, 256, launch<VD_T(Tile<2, 2, 2, 1, 512, 3>)>, 10.1f)         \
+  X(64, 64, 512, launch<VD_T(Tile<4, 2, 1, 2, 256, 4>)>, 11.5f)         \
+  X(64, 128, 512, launch<VD_T(Tile<2, 4, 2, 2, 256, 3>)>, 15.8f)        \
+  X(128, 128, 512, launch<VD_T(Tile<4, 2, 2, 4, 128, 4>)>, 21.9f)
 #define VD_T(...) __VA_ARGS__
 constexpr float kRoundT = 55.0f, kRoundU = 34.5f;  // of WideT and WideU
 
@@ -768,33 +782,36 @@ int run(const Call& x, hipStream_t stream) {
   const auto rounds = [&](int64_t tiles) { return (float)((tiles + geo.cus - 1) / geo.cus); };
   float best = 0.0f;
   int (*fn)(const Call&, hipStream_t) = nullptr;
-  const auto consider = [&](int bm, int bn, int (*f)(const Call&, hipStream_t), float round_us) {
-    const int64_t tiles_m = (x.M - 1) / bm + 1, tiles_n = (x.N - 1) / bn + 1;
-    if (tiles_m > (UINT32_MAX / 1024 - 8) / tiles_n) return;  // (a launch's threads are counted in 32 bits)
-    const float t = rounds(tiles_m * tiles_n) * round_us;
+  const auto consider = [&](int bm, int bn, int threads, int (*f)(const Call&, hipStream_t), float round_us) {
+    if (grid_blocks(x, bm, bn, threads, geo.xcds) < 0) return;
+    const float t = rounds(((x.M - 1) / bm + 1) * ((x.N - 1) / bn + 1)) * round_us;
     if (!fn || t < best) {
       best = t;
       fn = f;
     }
   };
-#define VD_FP8_CONSIDER(bm, bn, f, us) consider(bm, bn, &f, us);
+#define VD_FP8_CONSIDER(bm, bn, threads, f, us) consider(bm, bn, threads, &f, us);
   VD_FP8_SHAPES(VD_FP8_CONSIDER)
 #undef VD_FP8_CONSIDER
-  // (the wide tiles' rows lie within 32 bits of a descriptor's base)
-  if (fn && (x.lda >= kMaxWideStride || x.ldb >= kMaxWideStride)) return fn(x, stream);
-  // The wide tiles: all columns in tiles of T, or whole rounds of them and the columns
-  // behind in tiles of U, or all in U, whichever takes least.
-  const int64_t tiles_m = (x.M - 1) / WideT::BM + 1, all = (x.N - 1) / WideT::BN + 1;
-  if (tiles_m > (UINT32_MAX / WideT::kThreads - 64) / (2 * all)) return fn ? fn(x, stream) : VD_ERR_INVALID_ARG;
-  const auto wide_us = [&](int64_t tiles_t) {
-    const int64_t rest = x.N - tiles_t * WideT::BN;
-    return rounds(tiles_m * tiles_t) * kRoundT + (rest > 0 ? rounds(tiles_m * ((rest - 1) / WideU::BN + 1)) * kRoundU : 0.0f);
-  };
-  int64_t tiles_t = all;
-  for (const int64_t n : {tiles_m * all / geo.cus * geo.cus / tiles_m, (int64_t)0})
-    if (wide_us(n) < wide_us(tiles_t)) tiles_t = n;
-  if (fn && best <= wide_us(tiles_t)) return fn(x, stream);
-  return launch_wide(x, tiles_t, stream);
+  // The wide tiles (their rows lie within 32 bits of a descriptor's base): all columns in
+  // tiles of T, or whole rounds of them and the columns behind in tiles of U, or all in U,
+  // whichever takes least.
+  int64_t tiles_t = -1;
+  if (x.lda < kMaxWideStride && x.ldb < kMaxWideStride) {
+    const int64_t tiles_m = (x.M - 1) / WideT::BM + 1, all = (x.N - 1) / WideT::BN + 1;
+    const int64_t whole = tiles_m > INT64_MAX / all ? 0 : tiles_m * all / geo.cus * geo.cus / tiles_m;
+    for (const int64_t n : {all, whole, (int64_t)0}) {
+      const WideGrid g(x, n, geo);
+      if (!g.fits()) continue;
+      const float t = rounds(g.tiles_m * n) * kRoundT + rounds(g.tiles_m * g.tiles_u) * kRoundU;
+      if ((!fn && tiles_t < 0) || t < best) {
+        best = t;
+        tiles_t = n;
+      }
+    }
+  }
+  if (tiles_t >= 0) return launch_wide(x, tiles_t, stream);
+  return fn ? fn(x, stream) : VD_ERR_INVALID_ARG;
 }
 
 }  // namespace

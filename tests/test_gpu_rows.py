@@ -103,6 +103,15 @@ def test_rows_do_not_depend_on_the_call(k):
     assert o5 is xi and h5 is ri
     O.same_bits(xi, out)
     O.same_bits(ri, h)
+    xi, ri = x.clone(), r.clone()
+    V.rmsnorm(xi, w, EPS, residual=ri, residual_out=xi, out=ri)
+    O.same_bits(ri, out)
+    O.same_bits(xi, h)
+    xi, ri = x.clone(), r.clone()
+    q5, s5, h5 = V.rmsnorm_fp8(xi, w, EPS, residual=ri, residual_out=ri)
+    O.same_bits(q5, q)
+    O.same_bits(s5, s)
+    O.same_bits(ri, h)
     # strided rows in and out, scales row by row
     big = torch.zeros((m, k + 64), dtype=torch.bfloat16, device="cuda")
     big[:, 8:8 + k] = x
@@ -116,7 +125,7 @@ def test_rows_do_not_depend_on_the_call(k):
     assert (sc[:, 0] == 0).all() and (sc[:, 1 - (-k // 128):] == 0).all()
 
 
-@pytest.mark.parametrize("m,k", [(1024, 4104), (2077, 4104), (1025, 128), (40000, 200)])
+@pytest.mark.parametrize("m,k", [(1024, 4104), (2077, 4104), (1025, 128), (70000, 200)])
 def test_many_rows(m, k):
     """Calls whose rows go to the dies in runs and whose groups in tiles: every row has the bits
     of calls of 100 rows, and nothing behind the last row or group is written."""

@@ -96,6 +96,31 @@ def test_linear_fp8_rejects_before_launch(lib):
         assert call(K=k, lda=256, ldb=256) == -2, k
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="its pointers are not memory: without a "
+                    "device only the launches fail")
+@pytest.mark.parametrize("m,n,k,ld,want", [
+    (1, 1, 64, 64, -4), (1, 4096, 4096, 4096, -4), (48, 6144, 4096, 4096, -4),
+    (4096, 28672, 8192, 8192, -4), (4096, 6144, 4096, 2**24, -4), (2**22, 2**16, 0, 0, -4),
+    (2**30, 1, 0, 0, -4), (1, 2**30, 0, 0, -4), (2**26, 2**12, 64, 64, -4), (2**33, 1, 0, 0, -1),
+    (2**28, 2**16, 64, 2**24, -1), (2**40, 1, 0, 0, -1), (2**62, 2**31 - 1, 0, 0, -1),
+    (1, 1, 2**31 - 64, 2**29, -1)])
+def test_linear_fp8_launches_or_refuses_every_size(lib, m, n, k, ld, want):
+    """A call of any size launches a kernel or is refused: without a device a launch is
+    reported as failed, never VD_OK."""
+    got = lib.vd_linear_fp8(FAKE, ld, FAKE, 1, 2**40, FAKE, ld, FAKE, 1, 2**40, FAKE, n, m, n, k, None)
+    assert got == want
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="its pointers are not memory")
+@pytest.mark.parametrize("m,k", [(1, 8), (1, 32768), (2**20, 520), (2**27, 8), (2**40, 16)])
+def test_row_operators_launch(lib, m, k):
+    """As above: the norm of any number of rows, the 8-bit rows up to 2^27 groups."""
+    assert lib.vd_rmsnorm(FAKE, k, FAKE, k, FAKE, 1e-5, FAKE, k, FAKE + 16, k, m, k, None) == -4
+    assert lib.vd_rmsnorm_fp8(FAKE, k, None, 0, FAKE, 1e-5, None, 0, FAKE, k, FAKE, 1, m, m, k, None) == -4
+    want = -4 if m * -(-k // 128) <= 2**27 else -1
+    assert lib.vd_quantize_fp8(FAKE, k, FAKE, k, FAKE, k, FAKE, 1, m, m, k, None) == want
+
+
 def test_map_pages_rejects_before_launch(lib):
     fields = dict(num_seqs=2, total_q_tokens=4, q_lens=FAKE, cached_lens=FAKE + 64,
                   free_pages=FAKE + 128, num_free=3, num_pages=8, page_table=FAKE + 256, pt_stride=4,
@@ -111,7 +136,7 @@ def test_map_pages_rejects_before_launch(lib):
         assert call(**{name: None}) == -1, name
         assert call(**{name: FAKE + 2}) == -1, name
     assert call(slot_mapping=FAKE + 644) == -1
-    for kw in (dict(num_seqs=-1), dict(total_q_tokens=-1), dict(total_q_tokens=2**31),
+    for kw in (dict(num_seqs=-1), dict(num_seqs=2**31 - 1), dict(total_q_tokens=-1), dict(total_q_tokens=2**31),
                dict(num_free=-1), dict(num_pages=-1), dict(pt_stride=0), dict(context_lens=FAKE),
                dict(context_lens=FAKE + 64), dict(status=FAKE), dict(status=FAKE + 64)):
         assert call(**kw) == -1, kw
