@@ -308,10 +308,10 @@ int vd_kv_write(const vd_attn* h, const void* k_new, const void* v_new,
  *   status[r]: 0, or the bit mask of why the request is refused:
  *     1  s < 0, c < 0 or n > 2^31 - 1;      2  ceil(n / 16) > pt_stride;
  *     4  the free list ends before its pages (it and every later request that needs a page);
- *     8  its rows end past total_q_tokens.
+ *     8  its rows end past total_q_tokens (cu_q_lens[r + 1] > total_q_tokens, for s = 0 too).
  * A refused request takes no page, its table row is left as it was, its context_lens is 0 (the
  * attention skips it) and its rows' slots are -1 (the KV write skips them).  A request without
- * new tokens (s = 0) is not refused; the attention skips it.
+ * new tokens (s = 0) needs no page; the attention skips it whether it is refused or not.
  * All pointers are device memory, int32 arrays 4-byte and slot_mapping 8-byte aligned.  The
  * outputs overlap nothing else (context_lens or status == cached_lens or q_lens:
  * VD_ERR_INVALID_ARG).  One launch on `stream`, no workspace; it may be captured, and a replay

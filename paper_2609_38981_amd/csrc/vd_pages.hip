@@ -175,8 +175,8 @@ void launch(const vd_page_map& m, uint32_t num_free, hipStream_t stream) {
 }  // namespace
 
 extern "C" int vd_map_pages(const vd_page_map* m, hipStream_t stream) {
-  if (!m || m->num_seqs < 0 || m->num_seqs > INT32_MAX - 4096 || m->total_q_tokens < 0 || m->total_q_tokens > INT32_MAX - 4096 ||
-      m->num_free < 0 || m->num_pages < 0)
+  if (!m || m->num_seqs < 0 || m->num_seqs > INT32_MAX - 4096 || m->total_q_tokens < 0 ||
+      m->total_q_tokens > INT32_MAX - 4096 || m->num_free < 0 || m->num_pages < 0)
     return VD_ERR_INVALID_ARG;
   const auto bad = [](const void* p, bool needed, int n) {
     return (needed && !p) || (uintptr_t)p % n != 0;

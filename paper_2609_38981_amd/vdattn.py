@@ -443,6 +443,7 @@ def linear(a: torch.Tensor, b: torch.Tensor, out: Optional[torch.Tensor] = None,
 # ---------------------------------------------------------------------------
 E4M3 = torch.float8_e4m3fn
 SCALE_BLOCK = 128  # values per scale
+_INT32_MAX = 2 ** 31 - 1  # of the C arguments that are int32 (ctypes would cut a larger value)
 
 
 # The handle of a device's current stream (what torch.cuda.current_stream().cuda_stream gives)
@@ -477,13 +478,13 @@ def _device_of(t, name: str) -> int:
 
 
 def _rows(t, name: str, dtype, device: int, shape=None):
-    """Checks a 2-D tensor on ``device`` whose rows are contiguous (they may be strided); its
-    shape and row stride (a single row has none of its own)."""
+    """Checks a 2-D tensor on ``device`` whose rows are contiguous (they may be strided) and of
+    at most 2^31 - 1 values; its shape and row stride (a single row has none of its own)."""
     try:
         rows, cols = got = t.shape
         ld, step = t.stride()
         if t.dtype is dtype and (step == 1 or cols <= 1) and t.get_device() == device and (
-                shape is None or got == shape):
+                cols <= _INT32_MAX if shape is None else got == shape):
             return rows, cols, ld if rows > 1 else (cols + 15) // 16 * 16
     except (AttributeError, ValueError):
         pass
@@ -493,7 +494,7 @@ def _rows(t, name: str, dtype, device: int, shape=None):
         raise ValueError("%s must be on device %d" % (name, device))
     if shape is not None and t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    raise ValueError("%s must be 2-D with contiguous rows" % name)
+    raise ValueError("%s must be 2-D with contiguous rows of less than 2^31 values" % name)
 
 
 def _scales(s, name: str, rows: int, K: int, device: int):
@@ -537,6 +538,8 @@ def linear_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
     N, Kb, ldb = _rows(b, "b", E4M3, dev)
     if Kb != K:
         raise ValueError("a is [M, %d] but b is [N, %d]" % (K, Kb))
+    if N > _INT32_MAX:
+        raise ValueError("b must have less than 2^31 rows")
     a_strides = _scales(a_scales, "a_scales", M, K, dev)
     b_strides = _scales(b_scales, "b_scales", -(-N // SCALE_BLOCK), K, dev)
     if out is None:
@@ -652,6 +655,8 @@ def map_pages(q_lens: torch.Tensor, cached_lens: torch.Tensor, free_pages: torch
         raise ValueError("q_lens and cached_lens must be [num_seqs]")
     if page_table.dim() != 2 or page_table.size(0) != B:
         raise ValueError("page_table must be [num_seqs, stride]")
+    if max(page_table.shape) > _INT32_MAX:
+        raise ValueError("page_table must have less than 2^31 rows and columns")
     if out is None:
         cu, ctx, status, used = torch.empty(3 * B + 2, dtype=torch.int32, device=page_table.device).split(
             (B + 1, B, B, 1))

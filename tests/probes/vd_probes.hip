@@ -18,6 +18,10 @@
 //                  from lane 0 (the split launch's slot claims); out [wgs *
 //                  per] int32 gets them in claim order, counter [1] int32 is
 //                  zeroed by a fill launch first.
+//   vdp_buffer_copy: one wavefront: two copies of 16 bytes a lane into LDS through a buffer
+//                  descriptor of `bytes` bytes at src, lane l from byte l * step + soff (and
+//                  l * step + soff2); out [2][64][4] int32 gets the LDS, filled with -1 before.
+//                  size: the bytes that src has, past the descriptor's range too.
 //
 // Every entry point returns 0, or -1 for a bad size or pointer (nothing is
 // launched then), or -2 if the launch failed.  One wavefront per tile or per
@@ -25,6 +29,8 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+
+#include "../../paper_2609_38981_amd/csrc/vd_hw.hpp"
 
 namespace {
 
@@ -119,6 +125,18 @@ __global__ __launch_bounds__(64) void claims_kernel(int32_t* c, int32_t* out, in
   }
 }
 
+__global__ __launch_bounds__(64) void buffer_copy_kernel(const void* src, uint32_t bytes, uint32_t step,
+                                                         uint32_t soff, uint32_t soff2, int32_t* out) {
+  __shared__ __attribute__((aligned(16))) int32_t lds[512];
+  for (int i = 0; i < 8; ++i) lds[64 * i + threadIdx.x] = -1;
+  __syncthreads();
+  vd::lds_dma16_pair(vd::buffer_of((uint64_t)src, bytes), threadIdx.x * step, soff, soff2,
+                     (uint32_t)(uintptr_t)lds);
+  vd::wait_vmcnt<0>();
+  __syncthreads();
+  for (int i = 0; i < 8; ++i) out[64 * i + threadIdx.x] = lds[64 * i + threadIdx.x];
+}
+
 int launched() { return hipGetLastError() == hipSuccess ? 0 : -2; }
 
 }  // namespace
@@ -173,6 +191,17 @@ int vdp_claims(void* counter, void* out, int wgs, int per, hipStream_t stream) {
   hipLaunchKernelGGL(zero_kernel, dim3(1), dim3(64), 0, stream, static_cast<int32_t*>(counter));
   hipLaunchKernelGGL(claims_kernel, dim3((unsigned)wgs), dim3(64), 0, stream,
                      static_cast<int32_t*>(counter), static_cast<int32_t*>(out), per);
+  return launched();
+}
+
+int vdp_buffer_copy(const void* src, int64_t size, int64_t bytes, int64_t step, int64_t soff,
+                    int64_t soff2, void* out, hipStream_t stream) {
+  if (!src || !out || size > UINT32_MAX || bytes < 0 || bytes > size || step < 16 || soff < 0 || soff2 < 0 ||
+      step > size || soff > size || soff2 > size)
+    return -1;
+  if (63 * step + (soff > soff2 ? soff : soff2) + 16 > size) return -1;
+  hipLaunchKernelGGL(buffer_copy_kernel, dim3(1), dim3(64), 0, stream, src, (uint32_t)bytes,
+                     (uint32_t)step, (uint32_t)soff, (uint32_t)soff2, static_cast<int32_t*>(out));
   return launched();
 }
 

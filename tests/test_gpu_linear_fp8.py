@@ -4,6 +4,9 @@ invariance across the number of rows, positions, strides and the scales' layout,
 and edge cases."""
 from __future__ import annotations
 
+import ctypes
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -244,3 +247,42 @@ def test_wrapper_refuses():
                                                                        dtype=torch.bfloat16)), ValueError)]:
         with pytest.raises(e):
             f()
+
+
+def test_wrapper_refuses_sizes_past_31_bits():
+    """2^32 + 128 rows or columns would be 128 to a 32-bit argument."""
+    def codes(m, k):
+        return torch.empty((m, k), dtype=V.E4M3, device="cuda")
+
+    def scales(m, k):
+        return torch.empty((m, k), device="cuda")
+    n = 2**32 + 128
+    with pytest.raises(ValueError):
+        V.linear_fp8(codes(1, 0), scales(1, 0), codes(n, 0), scales(n // 128, 0))
+    with pytest.raises(ValueError):
+        V.linear_fp8(codes(0, n), scales(0, n // 128), codes(0, n), scales(0, n // 128))
+
+
+@pytest.mark.parametrize("bytes_,step,soff,soff2", [
+    (1 << 20, 16, 0, 1024),          # all in range
+    (1024, 16, 256, 512),            # the lanes' offsets in range, their sums with soff not all
+    (512, 16, 0, 496),
+    (512, 16, 512, 528),             # soff at the end, and past it
+    (512, 64, 8192, 4096),
+    (0, 16, 0, 16),
+    (128, 4096, 8 * 4096, 16 * 4096),  # one row of 128 bytes, rows 8 and 16 rows further
+    (9 * 4096 + 128, 4096, 8 * 4096, 16 * 4096)])
+def test_what_a_buffer_copy_reads_past_its_range(bytes_, step, soff, soff2):
+    """Nothing: zeros reach LDS where the lane's offset plus the instruction's lies past the
+    range (the memory behind it is the test's own)."""
+    lib = ctypes.CDLL(os.path.join(os.path.dirname(os.path.abspath(__file__)), "probes", "libvdprobes.so"))
+    i64, p = ctypes.c_int64, ctypes.c_void_p
+    lib.vdp_buffer_copy.argtypes = [p, i64, i64, i64, i64, i64, p, p]
+    src = torch.arange(1, (1 << 18) + 1, dtype=torch.int32, device="cuda")
+    out = torch.empty((2, 64, 4), dtype=torch.int32, device="cuda")
+    assert lib.vdp_buffer_copy(src.data_ptr(), 1 << 20, bytes_, step, soff, soff2, out.data_ptr(),
+                               torch.cuda.current_stream().cuda_stream) == 0
+    at = np.arange(64)[None] * step + np.array([soff, soff2])[:, None]
+    words = src.cpu().numpy()[at[..., None] // 4 + np.arange(4)]
+    want = np.where((at + 16 <= bytes_)[..., None], words, 0)
+    assert np.array_equal(out.cpu().numpy(), want)

@@ -152,3 +152,11 @@ def test_wrapper_refuses():
                  (lambda: V.map_pages(i, i, i, t, 4, 3, out=V.PageMap(i, i, i, i, i)), (TypeError, ValueError))]:
         with pytest.raises(e):
             f()
+
+
+def test_wrapper_refuses_a_table_past_31_bits():
+    """A row of 2^32 + 1 entries would be 1 to a 32-bit argument."""
+    i = _i32([1])
+    table = torch.empty((1, 2**32 + 1), dtype=torch.int32, device="cuda")  # 17 GB
+    with pytest.raises(ValueError):
+        V.map_pages(i, i, i, table, 4, 1)

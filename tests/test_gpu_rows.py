@@ -217,3 +217,12 @@ def test_wrappers_refuse():
     assert V.rmsnorm(x[:0], w).shape == (0, 128)
     q, s = V.quantize_fp8(x[:0])
     assert q.shape == (0, 128) and s.shape == (0, 1)
+
+
+def test_wrappers_refuse_rows_past_31_bits():
+    """2^32 + 128 columns would be 128 to a 32-bit argument."""
+    x = torch.empty((0, 2**32 + 128), dtype=torch.bfloat16, device="cuda")
+    w = torch.empty(2**32 + 128, dtype=torch.bfloat16, device="cuda")  # 8.6 GB
+    for f in (lambda: V.quantize_fp8(x), lambda: V.rmsnorm(x, w), lambda: V.rmsnorm_fp8(x, w)):
+        with pytest.raises(ValueError):
+            f()
